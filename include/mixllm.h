@@ -244,6 +244,150 @@ int mixllm_mixed_linear_fp16_static(const mixllm_desc *d, const void *x, const v
                                     const void *packed_w8, const void *scales4, const void *scales8,
                                     const void *zeros4, const int32_t *feature_perm, void *y, void *stream);
 
+/*
+ * The linear with what follows it in a block done on its fp32 sums, before the one rounding to fp16:
+ *   v[m][n] = sum_g float(P[m,n,g]) * s_w[n,g] * s_a[m,g] + bias[n]
+ *   y[m][n] = act(v[m][n]) + residual[m][n]                              (gated = 0)
+ *   y[m][i] = act(v[m][2 i]) * v[m][2 i + 1] + residual[m][i]            (gated = 1, y is [M][N / 2])
+ * Gated, the rows of W alternate: row 2 i is the gate and row 2 i + 1 the up value of output i, N and n8
+ * are even, and the list of 8-bit channels holds both rows of a pair or neither (the salience of a pair is
+ * that of its rows together).  A list that splits pairs leaves y unspecified (never an access out of bounds).
+ * The residual is added after the activation; `residual` may be y itself (added to in place).  Any of the
+ * parts may be absent; with all of them absent y is mixllm_mixed_linear's, up to fp32 rounding.
+ * Infinite or NaN values of bias and residual go through the formulas as they are.
+ */
+enum {
+    MIXLLM_ACT_NONE = 0,
+    MIXLLM_ACT_RELU = 1,     /* max(v, 0) */
+    MIXLLM_ACT_SILU = 2,     /* v / (1 + exp(-v)) */
+    MIXLLM_ACT_GELU = 3,     /* v (1 + erf(v / sqrt 2)) / 2 */
+    MIXLLM_ACT_GELU_TANH = 4 /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2 */
+};
+typedef struct mixllm_epilogue {
+    const void *bias;     /* fp16 [N], device, 2-byte aligned, or NULL */
+    const void *residual; /* fp16, of y's shape, device, 16-byte aligned, or NULL */
+    int32_t activation;   /* MIXLLM_ACT_* */
+    int32_t gated;        /* 0 or 1 */
+} mixllm_epilogue;
+
+/* mixllm_mixed_linear with an epilogue.  Same arguments, workspace and errors; EINVAL for an unknown activation or
+ * gated with an odd N or n8; EUNSUPPORTED beyond the tiled path's sizes (M K or the bytes of a part from 2^31 on). */
+int mixllm_mixed_linear_epilogue(const mixllm_desc *d, const int8_t *xq, const void *xscale,
+                                 const void *packed_w4, const void *packed_w8, const void *scales4,
+                                 const void *scales8, const void *zeros4, const int32_t *feature_perm,
+                                 const mixllm_epilogue *epilogue, void *y, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+/* mixllm_mixed_linear_fp16 with an epilogue: quantizer, linear and epilogue, in one kernel for a token or a few of a
+ * short row, otherwise in two.  Workspace and errors of mixllm_mixed_linear_fp16, and those above. */
+int mixllm_mixed_linear_fp16_epilogue(const mixllm_desc *d, const void *x, const void *packed_w4,
+                                      const void *packed_w8, const void *scales4, const void *scales8,
+                                      const void *zeros4, const int32_t *feature_perm,
+                                      const mixllm_epilogue *epilogue, void *y, void *workspace,
+                                      size_t workspace_bytes, void *stream);
+
+/*
+ * Router of a layer of experts.  An expert is selectable for a token when its logit is above -infinity (a NaN is
+ * not) and the token is not masked.  Scores over all experts of a token:
+ *   softmax  s_e = exp(l_e - max) / sum over the selectable ones   (logits of +infinity share 1 evenly)
+ *   sigmoid  s_e = 1 / (1 + exp(-l_e))
+ * Choice: c_e = s_e + bias_e, in 64 bits (a NaN or -infinity is not selectable).  With groups > 1 the experts fall
+ * into `groups` consecutive groups of E / groups; a group's score is its largest c_e, or the sum of its two largest,
+ * and only the experts of the top_groups groups with the largest scores stay selectable.  Of those the top_k largest
+ * c_e are taken, the largest first.  Ties go to the lowest index, of groups and of experts; equal are values that are equal
+ * as the real numbers above where there is neither a bias nor a sum of two, and their 64-bit values otherwise.
+ *   ids      [T][top_k]  the experts taken; -1 where fewer than top_k are selectable
+ *   weights  [T][top_k]  s_e of the experts taken (without the bias), 0 beside an id of -1; renormalize: divided by their
+ *                        sum (0 where that is 0); then times scale
+ * The assignments a = t top_k + j with an id, sorted by expert and then by a:
+ *   offsets  [E + 1]     offsets[e]: place of the first of expert e; offsets[E]: how many there are
+ *   rows     [T top_k]   rows[p] = the assignment at place p; -1 from place offsets[E] on
+ *   slots    [T][top_k]  place of assignment a; -1 where its id is -1
+ */
+enum { MIXLLM_SCORE_SOFTMAX = 0, MIXLLM_SCORE_SIGMOID = 1 };
+enum { MIXLLM_GROUP_MAX = 0, MIXLLM_GROUP_TOP2 = 1 };
+#define MIXLLM_MAX_EXPERTS 1024
+#define MIXLLM_MAX_TOP_K 32
+#define MIXLLM_MAX_EXPERT_GROUPS 64
+typedef struct mixllm_route_desc {
+    int32_t T;             /* tokens, 0 .. 2^24 */
+    int32_t E;             /* experts, 1 .. MIXLLM_MAX_EXPERTS */
+    int32_t top_k;         /* 1 .. min(E, MIXLLM_MAX_TOP_K) */
+    int32_t logits_fp16;   /* 1: logits are fp16, 0: fp32 */
+    int32_t logits_stride; /* elements from one token's logits to the next's, at least E */
+    int32_t score;         /* MIXLLM_SCORE_* */
+    int32_t groups;        /* 1 (none) .. MIXLLM_MAX_EXPERT_GROUPS, divides E */
+    int32_t top_groups;    /* 1 .. groups */
+    int32_t group_score;   /* MIXLLM_GROUP_* */
+    int32_t renormalize;   /* 0 or 1 */
+    float scale;
+} mixllm_route_desc;
+
+/* Bytes of scratch for the call below: 0 up to 64 tokens (one launch), 4 E for up to 256 blocks of tokens beyond (two). */
+size_t mixllm_route_workspace(const mixllm_route_desc *r);
+/*
+ *   logits     fp16 or fp32 [T][logits_stride], aligned to their elements
+ *   bias       fp32 [E], or NULL
+ *   mask       uint8 [T], 0 = a token that takes no expert (padding), or NULL
+ *   outputs as above; ids, offsets, rows, slots int32, weights fp32, all 4-byte aligned
+ *   workspace  4-byte aligned, mixllm_route_workspace() bytes (may be NULL when that is 0)
+ * T = 0 writes offsets only.  Errors: EINVAL, EUNSUPPORTED (beyond the limits above), EWORKSPACE, EHIP.
+ */
+int mixllm_route_experts(const mixllm_route_desc *r, const void *logits, const float *bias, const uint8_t *mask,
+                         int32_t *ids, float *weights, int32_t *offsets, int32_t *rows, int32_t *slots,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The linears of a layer of experts: E packed layers of one K, N and w8_group, each with its own set (and number) of
+ * 8-bit channels - to the global search an expert's linear is a layer like any other.  The library reaches them through
+ * a table in device memory that the caller keeps, together with the layers it points to.
+ *   mixllm_experts_table fills the table (mixllm_experts_table_bytes(E) bytes, 16-byte aligned) from HOST structs,
+ *   which are read before the call returns; asynchronous on `stream`.  Of d only K, N, group and w8_group are read.
+ */
+typedef struct mixllm_expert {
+    const void *packed_w4, *packed_w8, *scales4, *scales8, *zeros4; /* device, as for mixllm_mixed_linear */
+    const int32_t *feature_perm;
+    int32_t n8; /* 0..N */
+    int32_t reserved;
+} mixllm_expert;
+size_t mixllm_experts_table_bytes(int32_t E);
+int mixllm_experts_table(const mixllm_desc *d, int32_t E, const mixllm_expert *experts_host, void *table, void *stream);
+
+/*
+ * The products of the experts over the rows that a route gave them: for every expert e and place p in
+ * [offsets[e], offsets[e + 1]) the linear of expert e with its epilogue, from one row of activations to row p of y.
+ *   d             M = rows of xq; K, N, group, act_group, w8_group; n8 is not read
+ *   gather        top_k > 0: xq has a row per token, place p reads that of token rows[p] / top_k, and there are
+ *                 M top_k places (the first product); 0: xq has a row per place, there are M places and `rows` is not
+ *                 read (the second product)
+ *   offsets, rows what mixllm_route_experts leaves, or lists of the same form: offsets ascending from 0, at most the
+ *                 number of places.  They stay on the device, so their contents are not validated; places and tokens
+ *                 beyond the call's are clamped to it (results unspecified, never an access out of bounds).
+ *   epilogue      bias is [E][N] (or NULL), residual is NULL (it belongs to the sum, mixllm_experts_combine)
+ *   y             fp16 [places][N], gated [places][N / 2]; rows from offsets[E] on are left as they were
+ * Every row has the sums of mixllm_mixed_linear_epilogue on that row and expert, up to the order of the fp32 additions.
+ * Gated, N and every expert's n8 are even.
+ * Errors: EINVAL, EUNSUPPORTED (M K or a layer's bytes from 2^31 on; E beyond MIXLLM_MAX_EXPERTS), EHIP.
+ */
+int mixllm_experts_linear(const mixllm_desc *d, int32_t E, const void *table, const int8_t *xq, const void *xscale,
+                          const int32_t *offsets, const int32_t *rows, int32_t gather,
+                          const mixllm_epilogue *epilogue, void *y, void *stream);
+/* The same from fp16 activations x [M][K]: quantizer and products.  workspace: mixllm_experts_workspace(d) bytes for the
+ * codes and scales, 16-byte aligned. */
+size_t mixllm_experts_workspace(const mixllm_desc *d);
+int mixllm_experts_linear_fp16(const mixllm_desc *d, int32_t E, const void *table, const void *x,
+                               const int32_t *offsets, const int32_t *rows, int32_t gather,
+                               const mixllm_epilogue *epilogue, void *y, void *workspace, size_t workspace_bytes,
+                               void *stream);
+/*
+ * Weighted sum of the rows of every token's experts:
+ *   out[t][n] = residual[t][n] + sum_j weights[t][j] * y[slots[t][j]][n]      (fp32, in the order of j; one rounding)
+ * A slot of -1 adds nothing.  slots and weights int32 and fp32 [T][top_k] as mixllm_route_experts leaves them (a slot
+ * beyond the `places` rows of y adds nothing either); residual fp16 [T][N] or NULL, may be out itself.
+ * Errors: EINVAL, EUNSUPPORTED (top_k beyond MIXLLM_MAX_TOP_K), EHIP.
+ */
+int mixllm_experts_combine(int32_t T, int32_t top_k, int32_t N, int32_t places, const void *y, const float *weights,
+                           const int32_t *slots, const void *residual, void *out, void *stream);
+
 /* Same as mixllm_mixed_linear, with the kernel chosen by the caller (MIXLLM_PATH_*); for tests and benchmarks. */
 int mixllm_mixed_linear_path(const mixllm_desc *d, const int8_t *xq, const void *xscale,
                              const void *packed_w4, const void *packed_w8, const void *scales4,

@@ -41,6 +41,20 @@ class _Sizes(C.Structure):
                                           "y_bytes", "workspace_bytes", "linear_workspace_bytes")]
 
 
+class _Epilogue(C.Structure):
+    _fields_ = [("bias", C.c_void_p), ("residual", C.c_void_p), ("activation", C.c_int32), ("gated", C.c_int32)]
+
+
+class _RouteDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "E", "top_k", "logits_fp16", "logits_stride", "score", "groups", "top_groups",
+                                         "group_score", "renormalize")] + [("scale", C.c_float)]
+
+
+class _Expert(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("packed_w4", "packed_w8", "scales4", "scales8", "zeros4", "feature_perm")] + \
+               [("n8", C.c_int32), ("reserved", C.c_int32)]
+
+
 _lib = None
 _native = None
 _VP = C.c_void_p
@@ -77,9 +91,25 @@ def lib():
         L.mixllm_debug_check_fast_division.restype = C.c_int
         L.mixllm_debug_work_split.argtypes = [C.POINTER(_Desc), C.c_int, _VP]
         L.mixllm_debug_work_split.restype = C.c_int
+        L.mixllm_mixed_linear_epilogue.argtypes = [C.POINTER(_Desc)] + [_VP] * 8 + [C.POINTER(_Epilogue)] + [_VP] * 2 + [C.c_size_t, _VP]
+        L.mixllm_mixed_linear_fp16_epilogue.argtypes = [C.POINTER(_Desc)] + [_VP] * 7 + [C.POINTER(_Epilogue)] + [_VP] * 2 + [C.c_size_t, _VP]
+        L.mixllm_route_workspace.argtypes = [C.POINTER(_RouteDesc)]
+        L.mixllm_route_workspace.restype = C.c_size_t
+        L.mixllm_route_experts.argtypes = [C.POINTER(_RouteDesc)] + [_VP] * 9 + [C.c_size_t, _VP]
+        L.mixllm_experts_table_bytes.argtypes = [C.c_int32]
+        L.mixllm_experts_table_bytes.restype = C.c_size_t
+        L.mixllm_experts_table.argtypes = [C.POINTER(_Desc), C.c_int32, C.POINTER(_Expert), _VP, _VP]
+        L.mixllm_experts_workspace.argtypes = [C.POINTER(_Desc)]
+        L.mixllm_experts_workspace.restype = C.c_size_t
+        L.mixllm_experts_linear.argtypes = [C.POINTER(_Desc), C.c_int32] + [_VP] * 5 + [C.c_int32, C.POINTER(_Epilogue)] + [_VP] * 2
+        L.mixllm_experts_linear_fp16.argtypes = [C.POINTER(_Desc), C.c_int32] + [_VP] * 4 + [C.c_int32, C.POINTER(_Epilogue)] + \
+            [_VP] * 2 + [C.c_size_t, _VP]
+        L.mixllm_experts_combine.argtypes = [C.c_int32] * 4 + [_VP] * 6
         L.mixllm_channel_salience.restype = C.c_int
         L.mixllm_select_salient.restype = C.c_int
-        for name in ("mixllm_query_sizes", "mixllm_build_feature_perm", "mixllm_quantize_weights",
+        for name in ("mixllm_mixed_linear_epilogue", "mixllm_mixed_linear_fp16_epilogue", "mixllm_route_experts", "mixllm_experts_table",
+                     "mixllm_experts_linear", "mixllm_experts_linear_fp16", "mixllm_experts_combine",
+                     "mixllm_query_sizes", "mixllm_build_feature_perm", "mixllm_quantize_weights",
                      "mixllm_pack_weights", "mixllm_unpack_weights", "mixllm_quantize_activations",
                      "mixllm_mixed_linear", "mixllm_mixed_linear_path", "mixllm_debug_group_partials",
                      "mixllm_mixed_linear_fp16", "mixllm_mixed_linear_fp16_static", "mixllm_debug_channel_sums"):
@@ -90,7 +120,10 @@ def lib():
             raise MixllmError(f"{os.path.join(HERE, '_calls.so')} is missing or does not load ({e}): build it with "
                               "`python -m paper_2412_14590_amd.build` (there is no fallback)") from e
         _calls.bind(*(C.cast(f, _VP).value for f in (L.mixllm_query_sizes, L.mixllm_quantize_activations,
-                                                     L.mixllm_mixed_linear_path, L.mixllm_mixed_linear_fp16)))
+                                                     L.mixllm_mixed_linear_path, L.mixllm_mixed_linear_fp16,
+                                                     L.mixllm_mixed_linear_epilogue, L.mixllm_mixed_linear_fp16_epilogue,
+                                                     L.mixllm_route_workspace, L.mixllm_route_experts, L.mixllm_experts_workspace,
+                                                     L.mixllm_experts_linear, L.mixllm_experts_linear_fp16, L.mixllm_experts_combine)))
         _native = _calls
         _lib = L
     return _lib
@@ -302,6 +335,116 @@ def linear_fp16_static(x: torch.Tensor, L: PackedLayer, out: torch.Tensor, act_g
                                                  _ptr(L.z4), _ptr(L.perm), _ptr(out), _stream()),
            "mixllm_mixed_linear_fp16_static")
     return out
+
+
+ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+SCORES = {"softmax": 0, "sigmoid": 1}
+GROUP_SCORES = {"max": 0, "top2": 1}
+
+
+def _named(table: dict, name, what: str) -> int:
+    if name not in table:
+        raise ValueError(f"{what} is one of {', '.join(repr(n) for n in table)}, got {name!r}")
+    return table[name]
+
+
+def mixed_linear_epilogue(xq: torch.Tensor, xs: torch.Tensor, L: PackedLayer, bias=None, activation=None, gated: bool = False,
+                          residual=None, out=None, workspace=None) -> torch.Tensor:
+    """mixed_linear with bias [N], activation (ACTIVATIONS) and residual (of y's shape; may be `out` itself) done on its fp32 sums:
+    y = act(x W^T + bias) + residual.  gated: rows 2 i and 2 i + 1 of W are gate and up of output i, both 8-bit or neither, and
+    y [M, N/2] = act(gate) up + residual."""
+    return _result(_calls().mixed_linear_epilogue(xq, xs, L.K, L.N, L.n8, L.w8_group, L.w8, L.w4, L.s8, L.s4, L.z4, L.perm, bias, residual,
+                                                  _named(ACTIVATIONS, activation, "activation"), gated, out, workspace, _stream()),
+                   "mixllm_mixed_linear_epilogue")
+
+
+def linear_fp16_epilogue(x: torch.Tensor, L: PackedLayer, bias=None, activation=None, gated: bool = False, residual=None,
+                         act_group=None, out=None, workspace=None) -> torch.Tensor:
+    """linear_fp16 with the epilogue of mixed_linear_epilogue: fp16 x [M,K] in, fp16 y out, one kernel for a token."""
+    return _result(_calls().linear_fp16_epilogue(x, L.K, L.N, L.n8, L.w8_group, L.w8, L.w4, L.s8, L.s4, L.z4, L.perm,
+                                                 L.K if act_group is None else act_group, bias, residual,
+                                                 _named(ACTIVATIONS, activation, "activation"), gated, out, workspace, _stream()),
+                   "mixllm_mixed_linear_fp16_epilogue")
+
+
+@dataclass
+class Route:
+    """Which experts every token takes, and the assignments (token * top_k + j) sorted by expert."""
+    ids: torch.Tensor       # int32 [T, top_k], -1 = none
+    weights: torch.Tensor   # fp32 [T, top_k]
+    offsets: torch.Tensor   # int32 [E + 1]: place of every expert's first assignment
+    rows: torch.Tensor      # int32 [T * top_k]: assignment at every place, -1 behind the last
+    slots: torch.Tensor     # int32 [T, top_k]: place of every assignment, -1 = none
+
+
+def route_experts(logits: torch.Tensor, top_k: int, score: str = "softmax", bias=None, mask=None, groups: int = 1, top_groups: int = 1,
+                  group_score: str = "max", renormalize: bool = True, scale: float = 1.0) -> Route:
+    """Router: logits fp16 or fp32 [T,E] -> Route.  score "softmax" or "sigmoid"; bias fp32 [E] moves the choice, not the weights;
+    mask [T] (bool): False = padding; with groups > 1 only the experts of the top_groups best groups are chosen from, a group's
+    score being its best expert's ("max") or the sum of its two best ("top2").  An expert with a logit of -inf is never taken."""
+    return Route(*_result(_calls().route_experts(logits, top_k, _named(SCORES, score, "score"), bias, mask, groups, top_groups,
+                                                 _named(GROUP_SCORES, group_score, "group_score"), renormalize, scale, _stream()),
+                          "mixllm_route_experts"))
+
+
+@dataclass
+class PackedExperts:
+    """The packed layers of one linear of a layer of experts, and the device table through which the kernels reach them."""
+    K: int
+    N: int
+    w8_group: int
+    layers: list            # of PackedLayer: what the table points to
+    table: torch.Tensor
+
+    @property
+    def E(self) -> int:
+        return len(self.layers)
+
+
+def pack_experts(layers) -> PackedExperts:
+    """Packed layers of one K, N and w8_group (each with its own 8-bit channels) -> the experts of one linear."""
+    layers = list(layers)
+    assert layers and all((L.K, L.N, L.w8_group, L.perm.device) == (layers[0].K, layers[0].N, layers[0].w8_group, layers[0].perm.device)
+                          for L in layers), "experts of one size, granularity and device"
+    first = layers[0]
+    entries = (_Expert * len(layers))(*(_Expert(_ptr(L.w4), _ptr(L.w8), _ptr(L.s4), _ptr(L.s8), _ptr(L.z4), _ptr(L.perm), L.n8, 0)
+                                        for L in layers))
+    table = torch.empty(int(lib().mixllm_experts_table_bytes(len(layers))), dtype=torch.uint8, device=first.perm.device)
+    d = first.desc()
+    _check(lib().mixllm_experts_table(C.byref(d), len(layers), entries, _ptr(table), _stream()), "mixllm_experts_table")
+    return PackedExperts(first.K, first.N, first.w8_group, layers, table)
+
+
+def experts_linear(xq: torch.Tensor, xs: torch.Tensor, L: PackedExperts, route: Route, bias=None, activation=None, gated: bool = False,
+                   gather: bool = True, out=None) -> torch.Tensor:
+    """The linears of the experts over the rows routed to them: y [T * top_k, N] (gated [.., N/2]), one row per assignment in the
+    route's order; rows behind the last assignment are left as they were.  gather: xq has a row per token; otherwise one per
+    assignment, in the route's order.  bias fp16 [E,N]; activation and gated as in mixed_linear_epilogue."""
+    return _result(_calls().experts_linear(xq, xs, L.K, L.N, L.w8_group, L.E, L.table, route.offsets, route.rows, route.slots, gather, bias,
+                                           _named(ACTIVATIONS, activation, "activation"), gated, out, _stream()), "mixllm_experts_linear")
+
+
+def experts_linear_fp16(x: torch.Tensor, L: PackedExperts, route: Route, bias=None, activation=None, gated: bool = False,
+                        gather: bool = True, act_group=None, out=None, workspace=None) -> torch.Tensor:
+    """experts_linear from fp16 activations x [T,K] (gather) or [T * top_k, K]: quantizer and products."""
+    return _result(_calls().experts_linear_fp16(x, L.K, L.N, L.w8_group, L.E, L.table, route.offsets, route.rows, route.slots, gather,
+                                                L.K if act_group is None else act_group, bias,
+                                                _named(ACTIVATIONS, activation, "activation"), gated, out, workspace, _stream()),
+                   "mixllm_experts_linear_fp16")
+
+
+def experts_combine(y: torch.Tensor, route: Route, residual=None, out=None) -> torch.Tensor:
+    """Sum of every token's rows of y [T * top_k, N] by the route's weights, plus the residual [T,N] (may be `out` itself)."""
+    return _result(_calls().experts_combine(y, route.weights, route.slots, residual, out, _stream()), "mixllm_experts_combine")
+
+
+def experts_mlp(x: torch.Tensor, route: Route, gate_up: PackedExperts, down: PackedExperts, activation="silu", residual=None,
+                act_group=None, bias_gate_up=None, bias_down=None) -> torch.Tensor:
+    """A layer of experts: x [T,K] -> gated rows act(gate) up of every token's experts -> down -> their weighted sum + residual.
+    act_group: None (one activation scale per row) or 128, for both linears."""
+    h = experts_linear_fp16(x, gate_up, route, bias_gate_up, activation, gated=True, gather=True, act_group=act_group)
+    y = experts_linear_fp16(h, down, route, bias_down, gather=False, act_group=act_group)
+    return experts_combine(y, route, residual)
 
 
 def channel_salience(W: torch.Tensor, G: torch.Tensor, out=None, weight: float = 1.0, accumulate: bool = False) -> torch.Tensor:

@@ -16,7 +16,9 @@ LIB = os.environ.get("MIXLLM_LIB_OUT", os.path.join(HERE, "libmixllm_hip.so"))
 PROBE_LIB = os.path.join(HERE, "libmixllm_probe.so")
 CALLS = os.path.join(HERE, "_calls.so")   # the native part of the Python binding (binding.py)
 SOURCES = ["api.hip", "quant_act.hip", "quant_weights.hip", "linear_generic.hip",
-           "linear_decode.hip", "linear_decode_split.hip", "linear_mid.hip", "linear_prefill.hip", "salience.hip"]
+           "linear_decode.hip", "linear_decode_split.hip", "linear_mid.hip", "linear_prefill.hip", "salience.hip",
+           "epilogue_decode_split.hip", "epilogue_mid.hip", "epilogue_tiled.hip", "route.hip", "experts.hip"]
+HEADERS = [os.path.join(CSRC, h) for h in ("internal.h", "async_loads.h", "epilogue.h", "tiled.h", "decode_split.h", "mid.h", "experts.h")] + [os.path.join(INCLUDE, "mixllm.h")]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # correctly rounded fp32 division: the quantizers must match IEEE division bit for bit
@@ -34,9 +36,11 @@ def _hipcc():
 
 
 # sources with hand-issued loads -> the kernels in them that must not spill
-NO_SPILL = {"linear_prefill.hip": lambda n: "linear_prefill_kernel" in n or "linear_slices_kernel" in n,
-            "linear_decode_split.hip": lambda n: "linear_decode_split_kernel" in n,
-            "linear_mid.hip": lambda n: "linear_mid_kernel" in n}
+_TILED = lambda n: "linear_prefill_kernel" in n or "linear_slices_kernel" in n
+_SPLIT = lambda n: "linear_decode_split_kernel" in n
+_MID = lambda n: "linear_mid_kernel" in n
+NO_SPILL = {"linear_prefill.hip": _TILED, "epilogue_tiled.hip": _TILED, "linear_decode_split.hip": _SPLIT, "epilogue_decode_split.hip": _SPLIT,
+            "linear_mid.hip": _MID, "epilogue_mid.hip": _MID, "experts.hip": lambda n: "experts_tiled_kernel" in n}
 
 
 def _check_no_scratch(src: str, compile_log: str) -> None:
@@ -107,25 +111,26 @@ def check_hand_issued_loads(asm_text: str, name: str) -> None:
 # graph, loop back edges included).  The others issue or await some loads under conditions the scan cannot
 # relate to each other (the same uniform test before the load and before its wait), which it reports as
 # paths without a wait; they get the straight-line scan above and the tripwire below.
-FULL_SCAN = {"linear_prefill.hip"}
+FULL_SCAN = {"linear_prefill.hip", "epilogue_tiled.hip", "experts.hip"}
 # Kernels that keep a ring of hand-issued loads in flight around a rolled loop: registers of the ring must
 # stay where they are.  Where the loop nest makes the compiler rotate them (seen with the chunk loop of
 # the evenly split decode kernel nested in a loop over activation windows: 80 to 220 copies, at the loop
 # latch, of registers whose loads were still in flight; the late data then landed in registers that
 # held addresses by then) the kernel has dozens of register-to-register copies of them; as built it
 # has none, or a handful that copy a thread index into a register the ring used earlier.
-RING_COPY_LIMIT = {"linear_decode_split.hip": ("linear_decode_split_kernel", 8)}
+RING_COPY_LIMIT = {s: ("linear_decode_split_kernel", 8) for s in ("linear_decode_split.hip", "epilogue_decode_split.hip")}
 
 
 def check_ring_copies(asm_text: str, src: str) -> None:
     """Tripwire: count, per kernel, the VGPR-to-VGPR copies that name a destination register of a
     hand-issued load of the ring (the activation loads are consumed before the loop and their
-    registers reused); fail above RING_COPY_LIMIT."""
+    registers reused); fail above RING_COPY_LIMIT.  Where the source marks the ring as drained nothing is in flight
+    until the next of its loads: an epilogue there copies what it likes."""
     kernel, limit = RING_COPY_LIMIT[src]
     lines = asm_text.split("\n")
     for st in [i for i, l in enumerate(lines) if re.match(r"^_Z\S*" + kernel + r"\S*:", l)]:
         end = next((i for i in range(st, len(lines)) if "s_endpgm" in lines[i]), len(lines))
-        hand, copies, in_asm = set(), [], False
+        hand, copies, in_asm, drained = set(), [], False, False
         for l in lines[st:end]:
             t = l.strip()
             if t.startswith(";;#ASMSTART"):
@@ -133,8 +138,11 @@ def check_ring_copies(asm_text: str, src: str) -> None:
             elif t.startswith(";;#ASMEND"):
                 in_asm = False
             elif in_asm and (re.match(r"global_load_dwordx4 .* nt$", t) or t.startswith(("global_load_dwordx2", "global_load_ushort"))):
+                drained = False
                 hand |= _vregs(t.split(",")[0])   # weights (non-temporal) and their scales and zero points: the ring
-            elif re.match(r"v_(mov_b(32|64)_e32|swap_b32) v[\[\d][^,]*, v[\[\d]", t):
+            elif in_asm and t == "; ring drained":
+                drained = True
+            elif not drained and re.match(r"v_(mov_b(32|64)_e32|swap_b32) v[\[\d][^,]*, v[\[\d]", t):
                 copies.append(t)
         n = sum(1 for c in copies if _vregs(c) & hand)
         if n > limit:
@@ -151,7 +159,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
     objdir = os.path.join(HERE, "_build", "variant") if variant else os.path.join(HERE, "_build")
     force = force or variant
     os.makedirs(objdir, exist_ok=True)
-    deps = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "async_loads.h"), os.path.join(INCLUDE, "mixllm.h"), __file__]
+    deps = HEADERS + [__file__]
     dep_m = max(os.path.getmtime(p) for p in deps)
     objs, procs = [], []
     for src in SOURCES:
@@ -252,9 +260,7 @@ def build_sanitized_host(driver_cpp: str, exe: str) -> str:
     for src in SOURCES:
         s, o = os.path.join(CSRC, src), os.path.join(objdir, src.replace(".hip", ".o"))
         objs.append(o)
-        if not os.path.exists(o) or os.path.getmtime(o) < max(os.path.getmtime(p) for p in (s, os.path.join(CSRC, "internal.h"),
-                                                                                          os.path.join(CSRC, "async_loads.h"),
-                                                                                          os.path.join(INCLUDE, "mixllm.h"), __file__)):
+        if not os.path.exists(o) or os.path.getmtime(o) < max(os.path.getmtime(p) for p in (s, *HEADERS, __file__)):
             procs.append((src, subprocess.Popen([_hipcc(), *FLAGS, *san, "-c", s, "-o", o], stdout=subprocess.PIPE,
                                                 stderr=subprocess.STDOUT, text=True)))
     for src, pr in procs:

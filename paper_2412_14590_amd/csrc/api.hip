@@ -1,5 +1,6 @@
 // C ABI of libmixllm_hip.so: argument validation (host only, before anything is launched),
 // size accounting, feature permutation, and dispatch to the kernel launchers.
+#include <algorithm>
 #include <cstdlib>
 #include <mutex>
 #include <vector>
@@ -179,6 +180,39 @@ int auto_path(const mixllm_desc &d, const LinearParams &p)
     return (p.ng < 64 || split || wide) ? MIXLLM_PATH_PREFILL : MIXLLM_PATH_MID;
 }
 
+// The same choice for a call with an epilogue.  The one decode kernel that has it is the evenly split one; decode
+// shapes beyond that (3 or 4 tokens of a K so long that they do not fit the LDS stage) take the tiled kernel, and so do
+// those of the kernel for a few dozen tokens beyond 32, where an epilogue does not fit its registers.
+int auto_path_epilogue(const mixllm_desc &d, const LinearParams &p)
+{
+    const int path = auto_path(d, p);
+    const bool without = (path == MIXLLM_PATH_DECODE && !decode_split_covers(p)) || (path == MIXLLM_PATH_MID && d.M > 32);
+    return without ? MIXLLM_PATH_PREFILL : path;
+}
+
+int run_epilogue(const LinearParams &p, int path, hipStream_t st)
+{
+    switch (path) {
+    case PATH_SLICES: return hip_status(launch_slices_epilogue(p, st));
+    case MIXLLM_PATH_MID: return hip_status(launch_mid_epilogue(p, st));
+    case MIXLLM_PATH_PREFILL: return hip_status(launch_tiled_epilogue(p, st));
+    default: return hip_status(launch_split_epilogue(p, st));   // MIXLLM_PATH_DECODE
+    }
+}
+
+// Checks an epilogue against its linear and leaves it in the parameters.
+int set_epilogue(const mixllm_desc &d, const mixllm_epilogue *e, LinearParams &p)
+{
+    if (!e || e->activation < MIXLLM_ACT_NONE || e->activation > MIXLLM_ACT_GELU_TANH || (e->gated != 0 && e->gated != 1)) return MIXLLM_EINVAL;
+    if (e->gated && (d.N % 2 != 0 || d.n8 % 2 != 0)) return MIXLLM_EINVAL;
+    if (((uintptr_t)e->bias & 1u) || !aligned16(e->residual)) return MIXLLM_EINVAL;
+    p.ep.bias = (const half_t *)e->bias;
+    p.ep.residual = (const half_t *)e->residual;
+    p.ep.act = e->activation;
+    p.ep.gated = e->gated;
+    return MIXLLM_OK;
+}
+
 // Which kernel a call takes: the caller's path argument with AUTO resolved, or a negative status
 // when that path does not cover the shape.  Host arithmetic only; nothing is launched, so that a
 // call can refuse before it has enqueued anything.  `q` receives the parameters the launch uses.
@@ -340,14 +374,19 @@ int mixllm_quantize_activations(const mixllm_desc *d, const void *x, int8_t *xq,
     return hip_status(launch_quantize_activations(*d, x, xq, xscale, (hipStream_t)stream));
 }
 
-// Exactly one of y (the linear), P (per-group partial sums) and S (their sums over the groups) is given.
+// Exactly one of y (the linear), P (per-group partial sums) and S (their sums over the groups) is given; an epilogue (or
+// null) goes with y and the library's choice of kernel only.
 static int linear_common(const mixllm_desc *d, const int8_t *xq, const void *xscale, const void *packed_w4,
                          const void *packed_w8, const void *scales4, const void *scales8,
-                         const void *zeros4, const int32_t *feature_perm, void *y, int32_t *P, int32_t *S,
+                         const void *zeros4, const int32_t *feature_perm, const mixllm_epilogue *epilogue, void *y, int32_t *P, int32_t *S,
                          int path, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (int rc = check_desc(d)) return rc;
     if (path < MIXLLM_PATH_AUTO || path > MIXLLM_PATH_PREFILL_128) return MIXLLM_EINVAL;
+    if (epilogue) {
+        LinearParams checked{};
+        if (int rc = set_epilogue(*d, epilogue, checked)) return rc;
+    }
     if (d->M == 0) return MIXLLM_OK;
     mixllm_sizes s;
     sizes_of(*d, s);
@@ -368,7 +407,23 @@ static int linear_common(const mixllm_desc *d, const int8_t *xq, const void *xsc
         p.partials = (float *)workspace;
         p.partials_cap = workspace_bytes;
     }
+    if (epilogue) {
+        (void)set_epilogue(*d, epilogue, p);   // (checked above)
+        const int own = auto_path_epilogue(*d, p);
+        if (own == MIXLLM_PATH_PREFILL && !prefill_covers(p)) return MIXLLM_EUNSUPPORTED;
+        return run_epilogue(p, own, (hipStream_t)stream);
+    }
     return dispatch(*d, p, path, (hipStream_t)stream);
+}
+
+int mixllm_mixed_linear_epilogue(const mixllm_desc *d, const int8_t *xq, const void *xscale, const void *packed_w4,
+                                 const void *packed_w8, const void *scales4, const void *scales8, const void *zeros4,
+                                 const int32_t *feature_perm, const mixllm_epilogue *epilogue, void *y, void *workspace,
+                                 size_t workspace_bytes, void *stream)
+{
+    if (!epilogue) return MIXLLM_EINVAL;
+    return linear_common(d, xq, xscale, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm, epilogue, y,
+                         nullptr, nullptr, MIXLLM_PATH_AUTO, workspace, workspace_bytes, stream);
 }
 
 int mixllm_mixed_linear_path(const mixllm_desc *d, const int8_t *xq, const void *xscale,
@@ -376,7 +431,7 @@ int mixllm_mixed_linear_path(const mixllm_desc *d, const int8_t *xq, const void 
                              const void *scales8, const void *zeros4, const int32_t *feature_perm, void *y,
                              void *workspace, size_t workspace_bytes, int path, void *stream)
 {
-    return linear_common(d, xq, xscale, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm, y,
+    return linear_common(d, xq, xscale, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm, nullptr, y,
                          nullptr, nullptr, path, workspace, workspace_bytes, stream);
 }
 
@@ -393,9 +448,12 @@ int mixllm_mixed_linear(const mixllm_desc *d, const int8_t *xq, const void *xsca
 // and xscale between the quantizer and the linear where one kernel cannot do both.
 static int linear_from_fp16(const mixllm_desc *d, const void *x, const void *packed_w4, const void *packed_w8,
                             const void *scales4, const void *scales8, const void *zeros4, const int32_t *feature_perm,
-                            void *y, void *scratch, size_t scratch_bytes, hipStream_t st)
+                            const mixllm_epilogue *epilogue, void *y, void *scratch, size_t scratch_bytes, hipStream_t st)
 {
     if (int rc = check_desc(d)) return rc;
+    LinearParams checked{};
+    if (epilogue)
+        if (int rc = set_epilogue(*d, epilogue, checked)) return rc;
     if (d->M == 0) return MIXLLM_OK;
     mixllm_sizes s;
     sizes_of(*d, s);
@@ -405,12 +463,13 @@ static int linear_from_fp16(const mixllm_desc *d, const void *x, const void *pac
         return MIXLLM_EINVAL;
     LinearParams p = make_params(*d, nullptr, nullptr, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm);
     p.y = (half_t *)y;
+    p.ep = checked.ep;
     // One kernel when a decode variant can quantize inside the linear: every block then repeats the
     // quantizer, so the variants only offer it where that measured cheaper than the stand-alone
     // kernel's launch and round trips (one token; a few tokens of a short row).
     if (decode_can_fuse_quantizer(p)) {
         p.x = (const half_t *)x;
-        const int e = launch_linear_decode(p, st);
+        const int e = epilogue ? (decode_split_covers(p) ? launch_split_epilogue(p, st) : (int)hipErrorInvalidValue) : launch_linear_decode(p, st);
         if (e != (int)hipErrorInvalidValue) return hip_status(e);
         p.x = nullptr;   // no variant took the shape after all (nothing was launched): two kernels
     }
@@ -428,11 +487,12 @@ static int linear_from_fp16(const mixllm_desc *d, const void *x, const void *pac
         p.partials = (float *)((uint8_t *)scratch + quant_bytes);
         p.partials_cap = scratch_bytes - quant_bytes;
     }
-    LinearParams q;
-    const int path = resolve_path(*d, p, MIXLLM_PATH_AUTO, q);
+    LinearParams q = p;
+    int path = epilogue ? auto_path_epilogue(*d, p) : resolve_path(*d, p, MIXLLM_PATH_AUTO, q);
+    if (epilogue && path == MIXLLM_PATH_PREFILL && !prefill_covers(p)) path = MIXLLM_EUNSUPPORTED;
     if (path < 0) return path;
     if (int rc = hip_status(launch_quantize_activations(*d, x, xq, xscale, st))) return rc;
-    return run_path(q, path, st);
+    return epilogue ? run_epilogue(q, path, st) : run_path(q, path, st);
 }
 
 int mixllm_mixed_linear_fp16(const mixllm_desc *d, const void *x, const void *packed_w4, const void *packed_w8,
@@ -440,7 +500,17 @@ int mixllm_mixed_linear_fp16(const mixllm_desc *d, const void *x, const void *pa
                              const int32_t *feature_perm, void *y, void *workspace, size_t workspace_bytes,
                              void *stream)
 {
-    return linear_from_fp16(d, x, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm, y, workspace,
+    return linear_from_fp16(d, x, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm, nullptr, y, workspace,
+                            workspace_bytes, (hipStream_t)stream);
+}
+
+int mixllm_mixed_linear_fp16_epilogue(const mixllm_desc *d, const void *x, const void *packed_w4, const void *packed_w8,
+                                      const void *scales4, const void *scales8, const void *zeros4,
+                                      const int32_t *feature_perm, const mixllm_epilogue *epilogue, void *y, void *workspace,
+                                      size_t workspace_bytes, void *stream)
+{
+    if (!epilogue) return MIXLLM_EINVAL;
+    return linear_from_fp16(d, x, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm, epilogue, y, workspace,
                             workspace_bytes, (hipStream_t)stream);
 }
 
@@ -485,8 +555,172 @@ int mixllm_mixed_linear_fp16_static(const mixllm_desc *d, const void *x, const v
     hipError_t e = hipSuccess;
     void *area = static_scratch_ptr(&e);
     if (!area) return MIXLLM_EHIP;
-    return linear_from_fp16(d, x, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm, y, area,
+    return linear_from_fp16(d, x, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm, nullptr, y, area,
                             (size_t)MIXLLM_STATIC_SCRATCH_BYTES, (hipStream_t)stream);
+}
+
+static int check_route(const mixllm_route_desc *r)
+{
+    if (!r || r->T < 0 || r->E <= 0 || r->top_k <= 0 || r->top_k > r->E || r->groups <= 0 || r->E % r->groups != 0) return MIXLLM_EINVAL;
+    if (r->top_groups <= 0 || r->top_groups > r->groups || r->logits_stride < r->E) return MIXLLM_EINVAL;
+    if (r->score != MIXLLM_SCORE_SOFTMAX && r->score != MIXLLM_SCORE_SIGMOID) return MIXLLM_EINVAL;
+    if (r->group_score != MIXLLM_GROUP_MAX && r->group_score != MIXLLM_GROUP_TOP2) return MIXLLM_EINVAL;
+    if ((r->logits_fp16 != 0 && r->logits_fp16 != 1) || (r->renormalize != 0 && r->renormalize != 1)) return MIXLLM_EINVAL;
+    if (r->E > MIXLLM_MAX_EXPERTS || r->top_k > MIXLLM_MAX_TOP_K || r->groups > MIXLLM_MAX_EXPERT_GROUPS || r->T > (1 << 24))
+        return MIXLLM_EUNSUPPORTED;
+    return MIXLLM_OK;
+}
+
+size_t mixllm_route_workspace(const mixllm_route_desc *r) { return check_route(r) == MIXLLM_OK ? route_workspace_bytes(r->T, r->E) : 0; }
+
+int mixllm_route_experts(const mixllm_route_desc *r, const void *logits, const float *bias, const uint8_t *mask, int32_t *ids,
+                         float *weights, int32_t *offsets, int32_t *rows, int32_t *slots, void *workspace,
+                         size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_route(r)) return rc;
+    auto words = [](const void *p) { return p != nullptr && ((uintptr_t)p & 3u) == 0; };
+    if (!words(offsets)) return MIXLLM_EINVAL;
+    if (r->T > 0) {
+        if (!logits || ((uintptr_t)logits & (r->logits_fp16 ? 1u : 3u)) || ((uintptr_t)bias & 3u)) return MIXLLM_EINVAL;
+        if (!words(ids) || !words(weights) || !words(rows) || !words(slots)) return MIXLLM_EINVAL;
+    }
+    const size_t need = route_workspace_bytes(r->T, r->E);
+    if (need > 0) {
+        if (!words(workspace)) return MIXLLM_EINVAL;
+        if (workspace_bytes < need) return MIXLLM_EWORKSPACE;
+    }
+    RouteParams p{};
+    p.T = r->T;
+    p.E = r->E;
+    p.k = r->top_k;
+    p.half = r->logits_fp16;
+    p.ld = r->logits_stride;
+    p.sigmoid = r->score == MIXLLM_SCORE_SIGMOID;
+    p.groups = r->groups;
+    p.top_groups = r->top_groups;
+    p.group_top2 = r->group_score == MIXLLM_GROUP_TOP2;
+    p.renormalize = r->renormalize;
+    p.scale = r->scale;
+    p.logits = logits;
+    p.bias = bias;
+    p.mask = mask;
+    p.ids = ids;
+    p.weights = weights;
+    p.offsets = offsets;
+    p.rows = rows;
+    p.slots = slots;
+    p.counts = (int32_t *)workspace;
+    return hip_status(launch_route(p, (hipStream_t)stream));
+}
+
+size_t mixllm_experts_table_bytes(int32_t E) { return E > 0 ? (size_t)E * sizeof(ExpertEntry) : 0; }
+
+int mixllm_experts_table(const mixllm_desc *d, int32_t E, const mixllm_expert *experts_host, void *table, void *stream)
+{
+    if (!d || E <= 0 || !experts_host || !table || !aligned16(table)) return MIXLLM_EINVAL;
+    if (E > MIXLLM_MAX_EXPERTS) return MIXLLM_EUNSUPPORTED;
+    for (int32_t e = 0; e < E; ++e) {
+        const mixllm_expert &x = experts_host[e];
+        mixllm_desc own = *d;
+        own.M = 0;
+        own.n8 = x.n8;
+        own.act_group = d->K;
+        if (int rc = check_desc(&own)) return rc;
+        mixllm_sizes s;
+        sizes_of(own, s);
+        if (!buf_ok(x.packed_w8, s.w8_bytes) || !buf_ok(x.packed_w4, s.w4_bytes) || !buf_ok(x.scales8, s.scales8_bytes) ||
+            !buf_ok(x.scales4, s.scales4_bytes) || !buf_ok(x.zeros4, s.zeros4_bytes) || !buf_ok(x.feature_perm, s.perm_bytes))
+            return MIXLLM_EINVAL;
+    }
+    return hip_status(launch_experts_table(E, d->N, experts_host, (ExpertEntry *)table, (hipStream_t)stream));
+}
+
+// codes, then scales, of the experts' activations
+static size_t experts_scratch(const mixllm_desc &d, size_t &xq_bytes)
+{
+    mixllm_sizes s;
+    sizes_of(d, s);
+    xq_bytes = round_up_sz(s.xq_bytes, 256);
+    return xq_bytes + round_up_sz(s.xscale_bytes, 256);
+}
+
+static int check_experts_desc(const mixllm_desc *d)
+{
+    if (!d) return MIXLLM_EINVAL;
+    mixllm_desc own = *d;
+    own.n8 = 0;   // (not read: every expert has its own)
+    return check_desc(&own);
+}
+
+size_t mixllm_experts_workspace(const mixllm_desc *d)
+{
+    size_t xq_bytes;
+    return check_experts_desc(d) == MIXLLM_OK ? experts_scratch(*d, xq_bytes) : 0;
+}
+
+// Exactly one of (xq, xscale) and x is given.
+static int experts_common(const mixllm_desc *d0, int32_t E, const void *table, const int8_t *xq, const void *xscale, const void *x,
+                          const int32_t *offsets, const int32_t *rows, int32_t gather, const mixllm_epilogue *epilogue, void *y,
+                          void *workspace, size_t workspace_bytes, hipStream_t st)
+{
+    if (int rc = check_experts_desc(d0)) return rc;
+    mixllm_desc d = *d0;
+    d.n8 = 0;
+    if (E <= 0 || gather < 0 || gather > MIXLLM_MAX_TOP_K) return MIXLLM_EINVAL;
+    if (E > MIXLLM_MAX_EXPERTS) return MIXLLM_EUNSUPPORTED;
+    LinearParams p = make_params(d, xq, xscale, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
+    if (int rc = set_epilogue(d, epilogue, p)) return rc;
+    if (epilogue->residual) return MIXLLM_EINVAL;
+    if (d.M == 0) return MIXLLM_OK;
+    const long places = gather ? (long)d.M * gather : d.M;
+    if (!table || !aligned16(table) || !offsets || ((uintptr_t)offsets & 3u) || !y || !aligned16(y)) return MIXLLM_EINVAL;
+    if (gather && (!rows || ((uintptr_t)rows & 3u))) return MIXLLM_EINVAL;
+    if (!experts_cover(p)) return MIXLLM_EUNSUPPORTED;
+    if (x) {
+        size_t xq_bytes;
+        const size_t need = experts_scratch(d, xq_bytes);
+        if (!aligned16(x) || !workspace || !aligned16(workspace)) return MIXLLM_EINVAL;
+        if (workspace_bytes < need) return MIXLLM_EWORKSPACE;
+        p.xq = (const int8_t *)workspace;
+        p.xscale = (const half_t *)((uint8_t *)workspace + xq_bytes);
+    } else if (!xq || !aligned16(xq) || !xscale || !aligned16(xscale))
+        return MIXLLM_EINVAL;
+    p.y = (half_t *)y;
+    p.rows = gather ? rows : nullptr;
+    p.rows_per_token = std::max(gather, 1);
+    p.tokens = d.M;
+    ExpertsArgs a{(const ExpertEntry *)table, offsets, E, (int)places};
+    if (x)
+        if (int rc = hip_status(launch_quantize_activations(d, x, (int8_t *)p.xq, (void *)p.xscale, st))) return rc;
+    return hip_status(launch_experts_linear(p, a, st));
+}
+
+int mixllm_experts_linear(const mixllm_desc *d, int32_t E, const void *table, const int8_t *xq, const void *xscale,
+                          const int32_t *offsets, const int32_t *rows, int32_t gather, const mixllm_epilogue *epilogue, void *y,
+                          void *stream)
+{
+    return experts_common(d, E, table, xq, xscale, nullptr, offsets, rows, gather, epilogue, y, nullptr, 0, (hipStream_t)stream);
+}
+
+int mixllm_experts_linear_fp16(const mixllm_desc *d, int32_t E, const void *table, const void *x, const int32_t *offsets,
+                               const int32_t *rows, int32_t gather, const mixllm_epilogue *epilogue, void *y, void *workspace,
+                               size_t workspace_bytes, void *stream)
+{
+    if (!x && d && d->M > 0) return MIXLLM_EINVAL;
+    return experts_common(d, E, table, nullptr, nullptr, x, offsets, rows, gather, epilogue, y, workspace, workspace_bytes,
+                          (hipStream_t)stream);
+}
+
+int mixllm_experts_combine(int32_t T, int32_t top_k, int32_t N, int32_t places, const void *y, const float *weights,
+                           const int32_t *slots, const void *residual, void *out, void *stream)
+{
+    if (T < 0 || top_k <= 0 || N <= 0 || places < 0) return MIXLLM_EINVAL;
+    if (top_k > MIXLLM_MAX_TOP_K || T > (1 << 24) || N > (1 << 24)) return MIXLLM_EUNSUPPORTED;
+    if (T == 0) return MIXLLM_OK;
+    if ((places > 0 && (!y || !aligned16(y))) || !weights || ((uintptr_t)weights & 3u) || !slots || ((uintptr_t)slots & 3u) || !out ||
+        !aligned16(out) || !aligned16(residual))
+        return MIXLLM_EINVAL;
+    return hip_status(launch_experts_combine(T, top_k, N, places, y, weights, slots, residual, out, (hipStream_t)stream));
 }
 
 int mixllm_channel_salience(const mixllm_desc *d, const void *W, const void *G, float weight, int accumulate,
@@ -556,7 +790,7 @@ int mixllm_debug_group_partials(const mixllm_desc *d, const int8_t *xq, const vo
 {
     if (!P) return MIXLLM_EINVAL;
     return linear_common(d, xq, nullptr, packed_w4, packed_w8, nullptr, nullptr, zeros4, feature_perm,
-                         nullptr, P, nullptr, path, nullptr, 0, stream);
+                         nullptr, nullptr, P, nullptr, path, nullptr, 0, stream);
 }
 
 int mixllm_debug_channel_sums(const mixllm_desc *d, const int8_t *xq, const void *xscale, const void *packed_w4,
@@ -564,7 +798,7 @@ int mixllm_debug_channel_sums(const mixllm_desc *d, const int8_t *xq, const void
                               const void *zeros4, const int32_t *feature_perm, int32_t *S, int path, void *stream)
 {
     if (!S) return MIXLLM_EINVAL;
-    return linear_common(d, xq, xscale, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm, nullptr,
+    return linear_common(d, xq, xscale, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm, nullptr, nullptr,
                          nullptr, S, path, nullptr, 0, stream);
 }
 

@@ -1,0 +1,204 @@
+// The products of a layer of experts over the rows routed to them, and the weighted sum of every token's rows.
+//
+// The products run the tiles of the linear (tiled.h) - the same loads, matrix instructions, rescale and epilogue -
+// on one expert's packed layer and rows a block.  Rows come through the route's list (the activations of a token are
+// quantized and kept once, whatever the number of experts that read them) or lie one after another.  How many rows an
+// expert has is known on the device only: the grid covers the most tiles that the rows could make, and every
+// block finds its tile from the offsets by a sum over the experts.
+#include <algorithm>
+
+#include "experts.h"
+#include "tiled.h"
+
+namespace mixllm {
+
+namespace {
+
+constexpr int TABLE_CHUNK = 32;   // entries that travel as arguments of one launch
+struct TableChunk {
+    ExpertEntry entry[TABLE_CHUNK];
+};
+__global__ void experts_table_kernel(ExpertEntry *table, TableChunk chunk, int first, int n)
+{
+    if ((int)threadIdx.x < n) table[first + threadIdx.x] = chunk.entry[threadIdx.x];
+}
+
+// Logical tiles: those of the 4-bit parts of all experts, then those of the 8-bit parts; in a part expert by expert, the
+// row tiles of a column of channels next to each other.  As in the tiled kernel every XCD (blocks are dealt to them round
+// robin) takes a contiguous range of the 4-bit tiles, so that the blocks that share an expert's weights and rows share
+// an L2, and ends on its range of the cheaper 8-bit ones.
+template <typename C, bool ACT_PT, bool W8PC>
+__global__ __launch_bounds__(C::THREADS, 2) void experts_tiled_kernel(LinearParams p, ExpertsArgs a)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    using C8 = typename C::Half;
+    constexpr int T16 = C::BN / TILE_N;
+    const int lane = threadIdx.x & 63;
+    // tiles of expert e in either part
+    auto tiles_of = [&](int e, int &t4, int &t8) {
+        t4 = t8 = 0;
+        if (e < a.E) {
+            int first, count;
+            expert_rows(a, e, first, count);
+            t4 = (count + C::BM - 1) / C::BM * ((a.table[e].ntiles4 + T16 - 1) / T16);
+            t8 = (count + C8::BM - 1) / C8::BM * ((a.table[e].ntiles8 + T16 - 1) / T16);
+        }
+    };
+    int total4 = 0, total8 = 0;
+    for (int e0 = 0; e0 < a.E; e0 += 64) {
+        int t4, t8;
+        tiles_of(e0 + lane, t4, t8);
+        total4 += t4;
+        total8 += t8;
+    }
+    total4 = uniform(__shfl(wave_scan(total4), 63));
+    total8 = uniform(__shfl(wave_scan(total8), 63));
+    const int per4 = (total4 + 7) / 8, per8 = (total8 + 7) / 8;
+    const int xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
+    const bool part8 = i >= per4;
+    const int L = part8 ? xcd * per8 + (i - per4) : xcd * per4 + i;
+    if (part8 ? (i - per4 >= per8 || L >= total8) : L >= total4) return;
+    int e = 0, before = 0;
+    for (int e0 = 0, sum = 0; e0 < a.E; e0 += 64) {
+        int t4, t8;
+        tiles_of(e0 + lane, t4, t8);
+        const int own = part8 ? t8 : t4, upto = sum + wave_scan(own);
+        const unsigned long long here = __ballot(own > 0 && L >= upto - own && L < upto);
+        if (here) {
+            const int l = __ffsll(here) - 1;
+            e = uniform(e0 + l);
+            before = uniform(__shfl(upto - own, l));
+            break;
+        }
+        sum = uniform(__shfl(upto, 63));
+    }
+    const ExpertEntry &x = a.table[e];
+    int first, count;
+    expert_rows(a, e, first, count);
+    p.w4 = x.w4;
+    p.w8 = x.w8;
+    p.s4 = x.s4;
+    p.s8 = x.s8;
+    p.z4 = x.z4;
+    p.perm = x.perm;
+    p.n8 = x.n8;
+    p.n4 = x.n4;
+    p.ntiles8 = x.ntiles8;
+    p.ntiles4 = x.ntiles4;
+    p.M = count;
+    if (p.rows) p.rows += first;
+    else {
+        p.xq += (size_t)first * p.K;
+        p.xscale += (size_t)first * (ACT_PT ? 1 : p.ng);
+    }
+    p.y += (size_t)first * (p.ep.gated ? p.N / 2 : p.N);
+    if (p.ep.bias) p.ep.bias += (size_t)e * p.N;
+    const int BM = part8 ? C8::BM : C::BM;
+    const int nbm = (count + BM - 1) / BM, r = L - before, bn = r / nbm, bm = r - bn * nbm;
+    uint8_t *lds_a = smem;
+    float *lds_sa = (float *)(smem + NSTAGE * C::A_STAGE);
+    if (part8) {
+        if constexpr (W8PC && ACT_PT)
+            prefill_block_w8_channel_scale<C8, ACT_PT, 0, true, true>(p, bm * C8::BM, bn * T16, 0, p.ng, 0, lds_a, lds_sa, smem);
+        else
+            prefill_block<C8, 0, ACT_PT, true, !W8PC, true, true, true>(p, bm * C8::BM, bn * T16, 0, p.ng, 0, lds_a, lds_sa, smem);
+    } else
+        prefill_block<C, 0, ACT_PT, false, false, true, true, true>(p, bm * C::BM, bn * T16, 0, p.ng, 0, lds_a, lds_sa, smem);
+}
+
+template <typename C>
+int launch_experts_shape(const LinearParams &p, const ExpertsArgs &a, hipStream_t st)
+{
+    // the most tiles: every expert but those without rows has one that is not full; channel tiles of both parts of a layer
+    // whose parts are padded to 16
+    const long mt = a.places / C::Half::BM + std::min(a.E, a.places), nb = (p.N + 30) / C::BN + 2;
+    const long blocks = 8 * ((mt * nb + 7) / 8 + 2);
+    if (blocks >= (1l << 31)) return (int)hipErrorInvalidValue;
+    auto go = [&](auto kernel, bool grouped) {
+        const size_t lds = (size_t)NSTAGE * C::A_STAGE + token_scale_bytes(grouped, C::BM);
+        if (int e = ensure_dynamic_lds((const void *)kernel, lds)) return e;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(C::THREADS), lds, st, p, a);
+        return (int)hipGetLastError();
+    };
+    if (p.act_per_token) return p.w8_per_channel ? go(experts_tiled_kernel<C, true, true>, false) : go(experts_tiled_kernel<C, true, false>, false);
+    if constexpr (C::TM <= 2) return p.w8_per_channel ? go(experts_tiled_kernel<C, false, true>, true) : go(experts_tiled_kernel<C, false, false>, true);
+    return (int)hipErrorInvalidValue;
+}
+
+// One token's columns a thread: 8 where rows and columns allow 16-byte accesses, else one.
+template <int V>
+__global__ __launch_bounds__(256) void experts_combine_kernel(int T, int k, int N, int places, const half_t *y, const float *weights,
+                                                              const int32_t *slots, const half_t *residual, half_t *out)
+{
+    typedef half_t vec __attribute__((ext_vector_type(V)));
+    const int n = (blockIdx.x * 256 + threadIdx.x) * V, t = blockIdx.y;
+    if (n >= N) return;
+    float sum[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum[v] = 0.0f;
+    const size_t cell = (size_t)t * N + n;
+    vec res = {};
+    if (residual) res = *(const vec *)(residual + cell);
+    for (int j = 0; j < k; ++j) {
+        const int slot = slots[(size_t)t * k + j];
+        const float w = weights[(size_t)t * k + j];
+        if (slot < 0 || slot >= places) continue;
+        const vec row = *(const vec *)(y + (size_t)slot * N + n);
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] = __builtin_fmaf(w, (float)row[v], sum[v]);
+    }
+    vec o;
+#pragma unroll
+    for (int v = 0; v < V; ++v) o[v] = (half_t)(sum[v] + (float)res[v]);
+    *(vec *)(out + cell) = o;
+}
+
+}  // namespace
+
+int launch_experts_table(int E, int N, const mixllm_expert *experts, ExpertEntry *table, hipStream_t st)
+{
+    for (int e0 = 0; e0 < E; e0 += TABLE_CHUNK) {
+        TableChunk c{};
+        const int n = std::min(TABLE_CHUNK, E - e0);
+        for (int i = 0; i < n; ++i) {
+            const mixllm_expert &x = experts[e0 + i];
+            const int n4 = N - x.n8;
+            c.entry[i] = ExpertEntry{(const uint8_t *)x.packed_w4, (const int8_t *)x.packed_w8, (const half_t *)x.scales4, (const half_t *)x.scales8,
+                                     (const uint8_t *)x.zeros4, x.feature_perm, x.n8, n4, round_up(x.n8, TILE_N) / TILE_N, round_up(n4, TILE_N) / TILE_N};
+        }
+        hipLaunchKernelGGL(experts_table_kernel, dim3(1), dim3(64), 0, st, table, c, e0, n);
+        if (hipError_t err = hipGetLastError()) return (int)err;
+    }
+    return (int)hipSuccess;
+}
+
+// lanes address activations and one expert's weights and metadata with 32-bit byte offsets, whatever its share of 8-bit channels
+bool experts_cover(const LinearParams &p)
+{
+    const size_t lim = (size_t)1 << 31;
+    return (size_t)p.M * p.K < lim && (size_t)(p.N + 30) * p.K < lim;
+}
+
+int launch_experts_linear(const LinearParams &p, const ExpertsArgs &a, hipStream_t st)
+{
+    if (!experts_cover(p)) return (int)hipErrorInvalidValue;
+    if (a.places == 0) return (int)hipSuccess;
+    const long mean = a.places / a.E;   // rows of an expert
+    if (mean > 64 && p.act_per_token) return launch_experts_shape<Shape<1, 4, 4, MIXLLM_PREFILL_WD_LARGE>>(p, a, st);
+    if (mean > 24) return launch_experts_shape<Shape<1, 4, 2, MIXLLM_PREFILL_WD_SMALL>>(p, a, st);
+    return launch_experts_shape<Shape<1, 4, 1, MIXLLM_PREFILL_WD_SMALL>>(p, a, st);
+}
+
+int launch_experts_combine(int T, int k, int N, int places, const void *y, const float *weights, const int32_t *slots, const void *residual,
+                           void *out, hipStream_t st)
+{
+    if (T == 0) return (int)hipSuccess;
+    auto go = [&](auto kernel, int v) {
+        hipLaunchKernelGGL(kernel, dim3((N + 256 * v - 1) / (256 * v), T), dim3(256), 0, st, T, k, N, places, (const half_t *)y, weights, slots,
+                           (const half_t *)residual, (half_t *)out);
+        return (int)hipGetLastError();
+    };
+    return N % 8 == 0 ? go(experts_combine_kernel<8>, 8) : go(experts_combine_kernel<1>, 1);
+}
+
+}  // namespace mixllm

@@ -25,6 +25,14 @@ static inline __host__ __device__ int round_up(int a, int b) { return (a + b - 1
 // decode variants a caller can name through the path argument of the linear entry points
 enum DecodeVariant { DECODE_ANY = 0, DECODE_STREAM, DECODE_RESIDENT, DECODE_SPLIT };
 
+// what follows the product (epilogue.h); all zero where nothing does
+struct EpilogueArgs {
+    const half_t *bias;       // [N], or null
+    const half_t *residual;   // of y's shape, or null; may be y itself
+    int act;                  // MIXLLM_ACT_*
+    int gated;                // 1: channels 2 i and 2 i + 1 are gate and up of output i, y is [M][N / 2]
+};
+
 struct LinearParams {
     int M, K, N, n8, n4;
     int ng;         // K / 128
@@ -53,6 +61,11 @@ struct LinearParams {
     half_t *y;        // linear output, or
     int32_t *P;       // per-group partial sums [M][N][ng] (debug entry point), or
     int32_t *S;       // their sums over the groups [M][N] (debug entry point); exactly one of y / P / S is used
+    EpilogueArgs ep;  // kernels with an epilogue only
+    // experts' rows (kernels of the experts only): row m reads the activations of token rows[m] / rows_per_token, of `tokens` in
+    // all; rows null: of row m
+    const int32_t *rows;
+    int rows_per_token, tokens;
 };
 
 // ---- packed-layout addressing (see mixllm.h for the layout description) ----
@@ -243,6 +256,54 @@ bool prefill_plan(const LinearParams &p, int out[13]);
 // path for 17..128 tokens (linear_mid.hip)
 bool mid_covers(const LinearParams &p);
 int launch_linear_mid(const LinearParams &p, hipStream_t st);
+// the same kernels with an epilogue (p.ep); p.P and p.S are null
+int launch_split_epilogue(const LinearParams &p, hipStream_t st);
+int launch_mid_epilogue(const LinearParams &p, hipStream_t st);
+int launch_slices_epilogue(const LinearParams &p, hipStream_t st);
+int launch_tiled_epilogue(const LinearParams &p, hipStream_t st);
+// router (route.hip)
+struct RouteParams {
+    int T, E, k;
+    int half;              // logits: fp16 (1) or fp32
+    int ld;                // elements from one token's logits to the next's
+    int sigmoid;           // scores: sigmoid (1) or softmax
+    int groups, top_groups, group_top2;
+    int renormalize;
+    float scale;
+    const void *logits;
+    const float *bias;     // [E], or null
+    const uint8_t *mask;   // [T], or null
+    int32_t *ids;          // [T][k]
+    float *weights;        // [T][k]
+    int32_t *offsets;      // [E + 1]
+    int32_t *rows;         // [T k]
+    int32_t *slots;        // [T][k]
+    int32_t *counts;       // scratch: [blocks][E]
+};
+// experts (experts.hip): what an expert's packed layer is, in the device table
+struct ExpertEntry {
+    const uint8_t *w4;
+    const int8_t *w8;
+    const half_t *s4, *s8;
+    const uint8_t *z4;
+    const int32_t *perm;
+    int n8, n4;
+    int ntiles8, ntiles4;
+};
+struct ExpertsArgs {
+    const ExpertEntry *table;
+    const int32_t *offsets;   // [E + 1]
+    int E;
+    int places;               // rows of y at most
+};
+int launch_experts_table(int E, int N, const mixllm_expert *experts, ExpertEntry *table, hipStream_t st);
+bool experts_cover(const LinearParams &p);
+// p: M = rows of xq, rows / rows_per_token as the kernels read them (null: a row per place), the rest but the layer's own
+int launch_experts_linear(const LinearParams &p, const ExpertsArgs &a, hipStream_t st);
+int launch_experts_combine(int T, int k, int N, int places, const void *y, const float *weights, const int32_t *slots, const void *residual,
+                           void *out, hipStream_t st);
+size_t route_workspace_bytes(int T, int E);
+int launch_route(const RouteParams &p, hipStream_t st);
 // global precision search (salience.hip)
 int launch_channel_salience(const void *W, const void *Gr, int N, int K, float weight, int accumulate, float *salience,
                             hipStream_t st);

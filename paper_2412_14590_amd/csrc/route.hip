@@ -1,0 +1,382 @@
+// Router of a layer of experts: scores, a bias for balance, groups of experts, top-k, weights, and the lists of
+// rows per expert that the experts' products read.
+//
+// A token's experts are spread over LANES lanes (16 up to 256 experts, else a wave), SLOTS consecutive experts a
+// lane; the maxima over a token's lanes are rotations inside a row of 16 lanes (an instruction each).  The k experts
+// are found one after the other: the largest key, then the smallest index that has it, so that ties go to the lowest
+// index.  Keys are the logits themselves where score and choice have the same order (no bias, no sum of two scores),
+// which is exact; otherwise score + bias in 64 bits, because two experts whose 32-bit scores round alike are in
+// earnest in one batch of a few thousand tokens, and the choice would hang on the rounding of an exponential.
+//
+// The lists: a token takes an expert at most once, so the tokens of a group of 64 that took expert e are the bits of
+// one 64-bit word in LDS (an OR is the same in any order), the rank of an assignment among its expert's is a count of
+// the bits below its own, and the sorted order is that of the assignments' numbers without a sort.  Up to 64 tokens
+// one block does it all in one launch; beyond, the first launch leaves the counts of every block and expert, and the
+// second adds up those of the blocks before its own.
+#include <algorithm>
+#include <type_traits>
+
+#include "internal.h"
+
+namespace mixllm {
+
+namespace {
+
+constexpr int THREADS = 1024;
+// threads of a block of route_kernel: sixteen 64-bit keys a lane take more than the 128 registers of a block of 1024
+constexpr int threads_of(int slots, bool wide) { return slots == 16 && wide ? 512 : THREADS; }
+constexpr size_t LDS_CELLS = 140 * 1024;   // LDS for the keys of the waves' tokens, where groups are chosen
+constexpr int MAX_LIST_BLOCKS = 256;   // blocks that the tokens are cut into for counting (each reads the counts of all)
+
+template <int CTRL>
+__device__ inline float dpp(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true)); }
+template <int CTRL>
+__device__ inline int dpp(int v) { return __builtin_amdgcn_mov_dpp(v, CTRL, 0xf, 0xf, true); }
+template <int CTRL>
+__device__ inline double dpp(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint64_t lo = (uint32_t)dpp<CTRL>((int)(uint32_t)b), hi = (uint32_t)dpp<CTRL>((int)(uint32_t)(b >> 32));
+    return __builtin_bit_cast(double, lo | (hi << 32));
+}
+__device__ inline float at_lane(float v, int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l)); }
+__device__ inline int at_lane(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
+__device__ inline double at_lane(double v, int l)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint64_t lo = (uint32_t)at_lane((int)(uint32_t)b, l), hi = (uint32_t)at_lane((int)(uint32_t)(b >> 32), l);
+    return __builtin_bit_cast(double, lo | (hi << 32));
+}
+// op over the LANES lanes of a token; every lane gets the result (all lanes of the wave are active)
+template <int LANES, typename T, typename F>
+__device__ inline T over_token(T v, F &&op)
+{
+    v = op(v, dpp<0x121>(v));   // row_ror:1, 2, 4, 8
+    v = op(v, dpp<0x122>(v));
+    v = op(v, dpp<0x124>(v));
+    v = op(v, dpp<0x128>(v));
+    if constexpr (LANES == 64) v = op(op(at_lane(v, 0), at_lane(v, 16)), op(at_lane(v, 32), at_lane(v, 48)));
+    return v;
+}
+struct Max {
+    __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
+    __device__ double operator()(double a, double b) const { return fmax(a, b); }
+};
+struct Min {
+    __device__ int operator()(int a, int b) const { return min(a, b); }
+};
+struct Sum {
+    template <typename T>
+    __device__ T operator()(T a, T b) const { return a + b; }
+};
+
+constexpr int LOWEST_BITS = (int)0xff800000u;
+__device__ inline float lowest() { return __builtin_bit_cast(float, LOWEST_BITS); }
+
+// One wave's tokens: 64 / LANES of them, from `t0` on; those from `t_end` on are none.  `cells`: this wave's LDS
+// (groups only): [token][E] keys and [token][groups] scores of groups.  Leaves ids and weights in memory and the
+// tokens' bits (counted from `t_base`) in `taken`.
+template <int LANES, int SLOTS, bool WIDE>
+__device__ inline void route_tokens(const RouteParams &p, int t0, int t_end, int t_base, double *cells, unsigned long long *taken)
+{
+    using Key = std::conditional_t<WIDE, double, float>;
+    const int lane = threadIdx.x & 63, sub = lane % LANES, in_wave = lane / LANES;
+    const int tok = t0 + in_wave;
+    const bool live = tok < t_end;
+    const int row = min(tok, t_end - 1);
+    const bool on = !p.mask || p.mask[row] != 0;
+    float l[SLOTS];
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        const int e = sub * SLOTS + s;
+        float v = lowest();
+        if (e < p.E) v = p.half ? (float)((const half_t *)p.logits)[(size_t)row * p.ld + e] : ((const float *)p.logits)[(size_t)row * p.ld + e];
+        l[s] = on && v > lowest() ? v : lowest();   // (a NaN is not greater)
+    }
+    float m = l[0];
+#pragma unroll
+    for (int s = 1; s < SLOTS; ++s) m = fmaxf(m, l[s]);
+    m = over_token<LANES>(m, Max{});
+    // exp(l - m); the largest logits give 1 where they are infinite, too
+    auto from_top = [&](float v) { return v == m ? 1.0 : exp((double)v - (double)m); };
+
+    Key c[SLOTS];
+    double total = 0.0;   // of a softmax over all experts, where it is needed
+    if constexpr (WIDE) {
+        if (!p.sigmoid) {
+            double part = 0.0;
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) {
+                c[s] = l[s] > lowest() ? from_top(l[s]) : 0.0;
+                part += c[s];
+            }
+            total = over_token<LANES>(part, Sum{});
+        }
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            double v = p.sigmoid ? 1.0 / (1.0 + exp(-(double)l[s])) : c[s] / total;
+            if (p.bias) v += (double)p.bias[min(sub * SLOTS + s, p.E - 1)];
+            c[s] = l[s] > lowest() && v > -HUGE_VAL ? v : -HUGE_VAL;
+        }
+    } else {
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) c[s] = l[s];
+        if (!p.sigmoid && !p.renormalize) {
+            float part = 0.0f;
+#pragma unroll
+            for (int s = 0; s < SLOTS; ++s) part += l[s] > lowest() ? (l[s] == m ? 1.0f : expf(l[s] - m)) : 0.0f;
+            total = over_token<LANES>(part, Sum{});
+        }
+    }
+
+    if (p.groups > 1) {
+        // the keys through LDS: a lane finds the score of a group, its rank among the groups, and takes the group's
+        // experts out where it is not among the first (the wave's own cells: no barrier between its lanes)
+        Key *mine = (Key *)cells + (size_t)in_wave * p.E;
+        double *scores = cells + (size_t)(64 / LANES) * p.E + (size_t)in_wave * p.groups;
+        const int size = p.E / p.groups;
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s)
+            if (sub * SLOTS + s < p.E) mine[sub * SLOTS + s] = c[s];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int g = sub; g < p.groups; g += LANES) {
+            double first = -HUGE_VAL, second = -HUGE_VAL;
+            for (int i = 0; i < size; ++i) {
+                const double v = (double)mine[g * size + i];
+                second = fmax(second, fmin(first, v));
+                first = fmax(first, v);
+            }
+            scores[g] = p.group_top2 && second > -HUGE_VAL ? first + second : first;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int g = sub; g < p.groups; g += LANES) {
+            const double own = scores[g];
+            int before = 0;
+            for (int o = 0; o < p.groups; ++o) before += scores[o] > own || (scores[o] == own && o < g);
+            if (before >= p.top_groups)
+                for (int i = 0; i < size; ++i) mine[g * size + i] = (Key)-HUGE_VAL;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) c[s] = sub * SLOTS + s < p.E ? mine[sub * SLOTS + s] : (Key)-HUGE_VAL;
+    }
+
+    int my_id = -1;
+    float my_logit = lowest();
+    for (int j = 0; j < p.k; ++j) {
+        Key best = c[0];
+        int at = 0;
+        float logit = l[0];
+#pragma unroll
+        for (int s = 1; s < SLOTS; ++s) {
+            const bool over = c[s] > best;
+            best = over ? c[s] : best;
+            at = over ? s : at;
+            logit = over ? l[s] : logit;
+        }
+        const Key top = over_token<LANES>(best, Max{});
+        const int e_mine = sub * SLOTS + at;
+        const int e = over_token<LANES>(best == top ? e_mine : 0x7fffffff, Min{});
+        const bool found = top > (Key)-HUGE_VAL;
+        const float of_e = over_token<LANES>(e == e_mine ? logit : lowest(), Max{});
+        if (sub == j && found) {
+            my_id = e;
+            my_logit = of_e;
+        }
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s)
+            if (sub * SLOTS + s == e) c[s] = (Key)-HUGE_VAL;
+    }
+
+    double w = 0.0;
+    if (my_id >= 0) w = p.sigmoid ? 1.0 / (1.0 + exp(-(double)my_logit)) : from_top(my_logit);
+    if (p.renormalize) {
+        const double sum = over_token<LANES>(w, Sum{});
+        w = sum > 0.0 ? w / sum : 0.0;
+    } else if (!p.sigmoid && my_id >= 0)
+        w /= total;
+    if (live && sub < p.k) {
+        p.ids[(size_t)tok * p.k + sub] = my_id;
+        p.weights[(size_t)tok * p.k + sub] = (float)(w * (double)p.scale);
+        if (my_id >= 0) atomicOr(&taken[my_id], 1ull << (tok - t_base));
+    }
+}
+
+// exclusive sums of n integers in LDS over all threads of the block, in place; returns the sum of all
+__device__ inline int block_scan(int *v, int n, int *wave_sums)
+{
+    int before = 0;
+    for (int i0 = 0; i0 < n; i0 += blockDim.x) {
+        const int i = i0 + threadIdx.x;
+        const int own = i < n ? v[i] : 0;
+        int x = own;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int y = __shfl_up(x, d);
+            if ((int)(threadIdx.x & 63) >= d) x += y;
+        }
+        if ((threadIdx.x & 63) == 63) wave_sums[threadIdx.x >> 6] = x;
+        __syncthreads();
+        int of_waves = 0, all = 0;
+        for (int w = 0; w < (int)blockDim.x / 64; ++w) {
+            if (w < (int)threadIdx.x >> 6) of_waves += wave_sums[w];
+            all += wave_sums[w];
+        }
+        if (i < n) v[i] = before + of_waves + x - own;
+        before += all;
+        __syncthreads();
+    }
+    return before;
+}
+
+// rows and slots of the assignments of 64 tokens from `t_base` on; base[e]: place of the first of expert e
+__device__ inline void place_assignments(const RouteParams &p, int t_base, int t_end, const unsigned long long *taken, const int *base)
+{
+    const int n = (min(t_end, t_base + 64) - t_base) * p.k;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const int a = t_base * p.k + i, tok = i / p.k;
+        const int e = p.ids[a];
+        int slot = -1;
+        if (e >= 0) {
+            slot = base[e] + __popcll(taken[e] & ((1ull << tok) - 1));
+            p.rows[slot] = a;
+        }
+        p.slots[a] = slot;
+    }
+}
+
+// ONE: all tokens (at most 64) in one block, which makes the lists too.  Otherwise block b takes `span` tokens (a
+// multiple of 64) and leaves how many of them took each expert in counts[b].
+template <int LANES, int SLOTS, bool WIDE, bool ONE>
+__global__ __launch_bounds__(threads_of(SLOTS, WIDE)) void route_kernel(RouteParams p, int span)
+{
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    unsigned long long *taken = (unsigned long long *)smem;   // [E]
+    int *count = (int *)(taken + p.E);                        // [E]
+    int *wave_sums = count + p.E + (p.E & 1);                 // [16]
+    constexpr int TPW = 64 / LANES;
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    double *cells = (double *)(wave_sums + 16) + (size_t)wave * TPW * (p.E + p.groups);
+    const int t_lo = blockIdx.x * span, t_hi = min(p.T, t_lo + span);
+    for (int e = threadIdx.x; e < p.E; e += blockDim.x) count[e] = 0;
+    for (int t = t_lo; t < t_hi; t += 64) {
+        for (int e = threadIdx.x; e < p.E; e += blockDim.x) taken[e] = 0;
+        __syncthreads();
+        for (int u = t + wave * TPW; u < min(t + 64, t_hi); u += waves * TPW)
+            route_tokens<LANES, SLOTS, WIDE>(p, u, min(t + 64, t_hi), t, cells, taken);
+        __syncthreads();
+        for (int e = threadIdx.x; e < p.E; e += blockDim.x) count[e] += __popcll(taken[e]);
+        if constexpr (!ONE) __syncthreads();
+    }
+    if constexpr (ONE) {
+        __syncthreads();
+        const int all = block_scan(count, p.E, wave_sums);
+        for (int e = threadIdx.x; e < p.E; e += blockDim.x) p.offsets[e] = count[e];
+        if (threadIdx.x == 0) p.offsets[p.E] = all;
+        // (ids are read back from memory: written by this block, before the barriers of the scan)
+        place_assignments(p, 0, p.T, taken, count);
+        for (int i = all + threadIdx.x; i < p.T * p.k; i += blockDim.x) p.rows[i] = -1;
+    } else {
+        for (int e = threadIdx.x; e < p.E; e += blockDim.x) p.counts[(size_t)blockIdx.x * p.E + e] = count[e];
+    }
+}
+
+__global__ __launch_bounds__(THREADS) void route_lists_kernel(RouteParams p, int span)
+{
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    unsigned long long *taken = (unsigned long long *)smem;   // [E]
+    int *base = (int *)(taken + p.E);                         // [E] all tokens' counts, then the offsets
+    int *before = base + p.E;                                 // [E] counts of the blocks before this one
+    int *wave_sums = before + p.E;                            // [16]
+    for (int e = threadIdx.x; e < p.E; e += blockDim.x) base[e] = before[e] = 0;
+    __syncthreads();
+    // every group of threads as wide as the experts adds up a part of the blocks (whole numbers: any order)
+    const int width = min(p.E, (int)blockDim.x), parts = blockDim.x / width, part = threadIdx.x / width;
+    if (part < parts)
+        for (int e = threadIdx.x % width; e < p.E; e += width) {
+            int all = 0, ahead = 0;
+#pragma unroll 8
+            for (int b = part; b < (int)gridDim.x; b += parts) {
+                const int n = p.counts[(size_t)b * p.E + e];
+                all += n;
+                ahead += b < (int)blockIdx.x ? n : 0;
+            }
+            atomicAdd(&base[e], all);
+            atomicAdd(&before[e], ahead);
+        }
+    __syncthreads();
+    const int all = block_scan(base, p.E, wave_sums);
+    if (blockIdx.x == 0) {
+        for (int e = threadIdx.x; e < p.E; e += blockDim.x) p.offsets[e] = base[e];
+        if (threadIdx.x == 0) p.offsets[p.E] = all;
+    }
+    for (int e = threadIdx.x; e < p.E; e += blockDim.x) base[e] += before[e];
+    const int t_lo = blockIdx.x * span, t_hi = min(p.T, t_lo + span);
+    for (int t = t_lo; t < t_hi; t += 64) {
+        for (int e = threadIdx.x; e < p.E; e += blockDim.x) taken[e] = 0;
+        __syncthreads();
+        const int n = (min(t_hi, t + 64) - t) * p.k;
+        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+            const int e = p.ids[t * p.k + i];
+            if (e >= 0) atomicOr(&taken[e], 1ull << (i / p.k));
+        }
+        __syncthreads();
+        place_assignments(p, t, t_hi, taken, base);
+        __syncthreads();
+        for (int e = threadIdx.x; e < p.E; e += blockDim.x) base[e] += __popcll(taken[e]);
+    }
+    // places behind the last assignment
+    for (long i = (long)t_lo * p.k + threadIdx.x; i < (long)t_hi * p.k; i += blockDim.x)
+        if (i >= all) p.rows[i] = -1;
+}
+
+// tokens of a block of the counting launch: whole groups of 64, in at most MAX_LIST_BLOCKS blocks
+int route_span(int T) { return 64 * ((T + 64 * MAX_LIST_BLOCKS - 1) / (64 * MAX_LIST_BLOCKS)); }
+
+template <int LANES, int SLOTS>
+int launch_lanes(const RouteParams &p, bool wide, hipStream_t st)
+{
+    constexpr int TPW = 64 / LANES;
+    const bool one = p.T <= 64;
+    // a wave for every TPW tokens, as many as a block holds; the lists want a few for the experts
+    const size_t wave_cells = p.groups > 1 ? (size_t)TPW * (p.E + p.groups) * sizeof(double) : 0;
+    const int most = threads_of(SLOTS, wide) / 64;
+    int waves = one ? std::min(most, std::max((p.T + TPW - 1) / TPW, (p.E + 63) / 64)) : most;
+    if (wave_cells) waves = std::min(waves, (int)(LDS_CELLS / wave_cells));
+    const int span = one ? 64 : route_span(p.T), blocks = one ? 1 : (p.T + span - 1) / span;
+    const size_t lds = (size_t)p.E * 8 + (size_t)(p.E + (p.E & 1)) * 4 + 64 + waves * wave_cells;
+    auto go = [&](auto kernel) {
+        if (lds > 48 * 1024)
+            if (int e = ensure_dynamic_lds((const void *)kernel, lds)) return e;
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64 * waves), lds, st, p, span);
+        return (int)hipGetLastError();
+    };
+    if (one) return wide ? go(route_kernel<LANES, SLOTS, true, true>) : go(route_kernel<LANES, SLOTS, false, true>);
+    if (int e = wide ? go(route_kernel<LANES, SLOTS, true, false>) : go(route_kernel<LANES, SLOTS, false, false>)) return e;
+    hipLaunchKernelGGL(route_lists_kernel, dim3(blocks), dim3(THREADS), (size_t)p.E * 16 + 64, st, p, span);
+    return (int)hipGetLastError();
+}
+
+}  // namespace
+
+size_t route_workspace_bytes(int T, int E)
+{
+    if (T <= 64) return 0;
+    const int span = route_span(T);
+    return (size_t)((T + span - 1) / span) * E * sizeof(int32_t);
+}
+
+int launch_route(const RouteParams &p, hipStream_t st)
+{
+    // 64-bit keys wherever the order of the choice is not that of the logits
+    const bool wide = p.bias || (p.groups > 1 && p.group_top2);
+    if (p.E <= 256 && p.k <= 16) {
+        if (p.E <= 64) return launch_lanes<16, 4>(p, wide, st);
+        if (p.E <= 128) return launch_lanes<16, 8>(p, wide, st);
+        return launch_lanes<16, 16>(p, wide, st);
+    }
+    if (p.E <= 256) return launch_lanes<64, 4>(p, wide, st);
+    return launch_lanes<64, 16>(p, wide, st);
+}
+
+}  // namespace mixllm
