@@ -322,14 +322,15 @@ typedef struct mixllm_route_desc {
     float scale;
 } mixllm_route_desc;
 
-/* Bytes of scratch for the call below: 0 up to 64 tokens (one launch), 4 E for up to 256 blocks of tokens beyond (two). */
+/* Bytes of scratch for the call below: 0 up to 16 tokens (one launch), beyond that 2 bytes per expert (rounded up to
+ * 8) for each of up to 256 blocks of tokens (two). */
 size_t mixllm_route_workspace(const mixllm_route_desc *r);
 /*
  *   logits     fp16 or fp32 [T][logits_stride], aligned to their elements
  *   bias       fp32 [E], or NULL
  *   mask       uint8 [T], 0 = a token that takes no expert (padding), or NULL
  *   outputs as above; ids, offsets, rows, slots int32, weights fp32, all 4-byte aligned
- *   workspace  4-byte aligned, mixllm_route_workspace() bytes (may be NULL when that is 0)
+ *   workspace  16-byte aligned, mixllm_route_workspace() bytes (may be NULL when that is 0)
  * T = 0 writes offsets only.  Errors: EINVAL, EUNSUPPORTED (beyond the limits above), EWORKSPACE, EHIP.
  */
 int mixllm_route_experts(const mixllm_route_desc *r, const void *logits, const float *bias, const uint8_t *mask,

@@ -586,7 +586,7 @@ int mixllm_route_experts(const mixllm_route_desc *r, const void *logits, const f
     }
     const size_t need = route_workspace_bytes(r->T, r->E);
     if (need > 0) {
-        if (!words(workspace)) return MIXLLM_EINVAL;
+        if (!workspace || !aligned16(workspace)) return MIXLLM_EINVAL;
         if (workspace_bytes < need) return MIXLLM_EWORKSPACE;
     }
     RouteParams p{};
@@ -609,7 +609,7 @@ int mixllm_route_experts(const mixllm_route_desc *r, const void *logits, const f
     p.offsets = offsets;
     p.rows = rows;
     p.slots = slots;
-    p.counts = (int32_t *)workspace;
+    p.counts = (uint16_t *)workspace;
     return hip_status(launch_route(p, (hipStream_t)stream));
 }
 

@@ -278,7 +278,8 @@ struct RouteParams {
     int32_t *offsets;      // [E + 1]
     int32_t *rows;         // [T k]
     int32_t *slots;        // [T][k]
-    int32_t *counts;       // scratch: [blocks][E]
+    uint16_t *counts;      // scratch: [blocks][Ep]
+    int Ep;                // E rounded up to 8
 };
 // experts (experts.hip): what an expert's packed layer is, in the device table
 struct ExpertEntry {

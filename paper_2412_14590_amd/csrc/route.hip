@@ -1,18 +1,21 @@
 // Router of a layer of experts: scores, a bias for balance, groups of experts, top-k, weights, and the lists of
 // rows per expert that the experts' products read.
 //
-// A token's experts are spread over LANES lanes (16 up to 256 experts, else a wave), SLOTS consecutive experts a
-// lane; the maxima over a token's lanes are rotations inside a row of 16 lanes (an instruction each).  The k experts
-// are found one after the other: the largest key, then the smallest index that has it, so that ties go to the lowest
-// index.  Keys are the logits themselves where score and choice have the same order (no bias, no sum of two scores),
-// which is exact; otherwise score + bias in 64 bits, because two experts whose 32-bit scores round alike are in
-// earnest in one batch of a few thousand tokens, and the choice would hang on the rounding of an exponential.
+// A token's experts are spread over LANES lanes, SLOTS consecutive experts a lane: a wave for every token, or, where
+// there are tokens enough to fill the chip, 16 lanes, whose maxima are rotations inside a row of lanes (an instruction
+// each) that serve four tokens at once.  The k experts are found one after the other: the largest key, then the smallest
+// index that has it, so that ties go to the lowest index.  Keys are the logits themselves where score and choice have the
+// same order (no bias, no sum of two scores), which is exact; otherwise score + bias in 64 bits, because two experts whose
+// 32-bit scores round alike are in earnest in one batch of a few thousand tokens, and the choice would hang on the rounding
+// of an exponential.
 //
 // The lists: a token takes an expert at most once, so the tokens of a group of 64 that took expert e are the bits of
 // one 64-bit word in LDS (an OR is the same in any order), the rank of an assignment among its expert's is a count of
-// the bits below its own, and the sorted order is that of the assignments' numbers without a sort.  Up to 64 tokens
+// the bits below its own, and the sorted order is that of the assignments' numbers without a sort.  Up to 16 tokens
 // one block does it all in one launch; beyond, the first launch leaves the counts of every block and expert, and the
 // second adds up those of the blocks before its own.
+//
+// Bound by instructions and latency, not by the logits' few bytes.
 #include <algorithm>
 #include <type_traits>
 
@@ -23,10 +26,11 @@ namespace mixllm {
 namespace {
 
 constexpr int THREADS = 1024;
+constexpr int MAX_BLOCKS = 256;   // blocks that the tokens are cut into for counting (a block of the lists reads the counts of all)
+constexpr int ONE_LAUNCH = 16;    // tokens up to which one block takes a wave for each
+constexpr size_t LDS_CELLS = 140 * 1024;   // LDS for the keys of the waves' tokens, where groups are chosen
 // threads of a block of route_kernel: sixteen 64-bit keys a lane take more than the 128 registers of a block of 1024
 constexpr int threads_of(int slots, bool wide) { return slots == 16 && wide ? 512 : THREADS; }
-constexpr size_t LDS_CELLS = 140 * 1024;   // LDS for the keys of the waves' tokens, where groups are chosen
-constexpr int MAX_LIST_BLOCKS = 256;   // blocks that the tokens are cut into for counting (each reads the counts of all)
 
 template <int CTRL>
 __device__ inline float dpp(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true)); }
@@ -61,6 +65,7 @@ __device__ inline T over_token(T v, F &&op)
 struct Max {
     __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
     __device__ double operator()(double a, double b) const { return fmax(a, b); }
+    __device__ int operator()(int a, int b) const { return max(a, b); }
 };
 struct Min {
     __device__ int operator()(int a, int b) const { return min(a, b); }
@@ -73,13 +78,35 @@ struct Sum {
 constexpr int LOWEST_BITS = (int)0xff800000u;
 __device__ inline float lowest() { return __builtin_bit_cast(float, LOWEST_BITS); }
 
+// Keys: scores in 64 bits, or the logits as whole numbers in the same order (a maximum of floats costs an instruction more
+// per operand, to quiet what might be a signalling NaN).
+template <bool WIDE>
+struct KeyOf {
+    using type = int;
+    static __device__ int none() { return (int)0x80000000u; }   // below any logit's
+    static __device__ int of(float l)
+    {
+        const int b = __builtin_bit_cast(int, l + 0.0f);   // (one zero)
+        return l > lowest() ? b ^ ((b >> 31) & 0x7fffffff) : none();
+    }
+    static __device__ float logit(int k) { return __builtin_bit_cast(float, k ^ ((k >> 31) & 0x7fffffff)); }
+    static __device__ double wide(int k) { return k == none() ? -HUGE_VAL : (double)logit(k); }
+};
+template <>
+struct KeyOf<true> {
+    using type = double;
+    static __device__ double none() { return -HUGE_VAL; }
+    static __device__ double wide(double k) { return k; }
+};
+
 // One wave's tokens: 64 / LANES of them, from `t0` on; those from `t_end` on are none.  `cells`: this wave's LDS
 // (groups only): [token][E] keys and [token][groups] scores of groups.  Leaves ids and weights in memory and the
 // tokens' bits (counted from `t_base`) in `taken`.
 template <int LANES, int SLOTS, bool WIDE>
 __device__ inline void route_tokens(const RouteParams &p, int t0, int t_end, int t_base, double *cells, unsigned long long *taken)
 {
-    using Key = std::conditional_t<WIDE, double, float>;
+    using KEY = KeyOf<WIDE>;
+    using Key = typename KEY::type;
     const int lane = threadIdx.x & 63, sub = lane % LANES, in_wave = lane / LANES;
     const int tok = t0 + in_wave;
     const bool live = tok < t_end;
@@ -120,7 +147,7 @@ __device__ inline void route_tokens(const RouteParams &p, int t0, int t_end, int
         }
     } else {
 #pragma unroll
-        for (int s = 0; s < SLOTS; ++s) c[s] = l[s];
+        for (int s = 0; s < SLOTS; ++s) c[s] = KEY::of(l[s]);
         if (!p.sigmoid && !p.renormalize) {
             float part = 0.0f;
 #pragma unroll
@@ -130,62 +157,80 @@ __device__ inline void route_tokens(const RouteParams &p, int t0, int t_end, int
     }
 
     if (p.groups > 1) {
-        // the keys through LDS: a lane finds the score of a group, its rank among the groups, and takes the group's
-        // experts out where it is not among the first (the wave's own cells: no barrier between its lanes)
+        // The keys through LDS: `width` neighbouring lanes (a power of two) find the score of a group, its rank among the
+        // groups, and take the group's experts out where it is not among the first.  (The wave's own cells: its LDS
+        // accesses are in order, no barrier.)
         Key *mine = (Key *)cells + (size_t)in_wave * p.E;
         double *scores = cells + (size_t)(64 / LANES) * p.E + (size_t)in_wave * p.groups;
         const int size = p.E / p.groups;
+        int width = 1;
+        while (2 * width * p.groups <= LANES) width *= 2;
+        const int part = sub & (width - 1), per_pass = LANES / width;   // groups at a time
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s)
             if (sub * SLOTS + s < p.E) mine[sub * SLOTS + s] = c[s];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        for (int g = sub; g < p.groups; g += LANES) {
+        for (int g0 = 0; g0 < p.groups; g0 += per_pass) {
+            const int g = g0 + sub / width;
             double first = -HUGE_VAL, second = -HUGE_VAL;
-            for (int i = 0; i < size; ++i) {
-                const double v = (double)mine[g * size + i];
-                second = fmax(second, fmin(first, v));
-                first = fmax(first, v);
+            if (g < p.groups) {
+#pragma unroll 4
+                for (int i = part; i < size; i += width) {
+                    const double v = KEY::wide(mine[g * size + i]);
+                    second = fmax(second, fmin(first, v));
+                    first = fmax(first, v);
+                }
             }
-            scores[g] = p.group_top2 && second > -HUGE_VAL ? first + second : first;
+            for (int d = 1; d < width; d *= 2) {
+                const double f = __shfl_xor(first, d), o = __shfl_xor(second, d);
+                second = fmax(fmax(second, o), fmin(first, f));
+                first = fmax(first, f);
+            }
+            if (g < p.groups && part == 0) scores[g] = p.group_top2 && second > -HUGE_VAL ? first + second : first;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        for (int g = sub; g < p.groups; g += LANES) {
-            const double own = scores[g];
+        for (int g0 = 0; g0 < p.groups; g0 += per_pass) {
+            const int g = g0 + sub / width;
+            const double own = scores[min(g, p.groups - 1)];
             int before = 0;
-            for (int o = 0; o < p.groups; ++o) before += scores[o] > own || (scores[o] == own && o < g);
-            if (before >= p.top_groups)
-                for (int i = 0; i < size; ++i) mine[g * size + i] = (Key)-HUGE_VAL;
+#pragma unroll 4
+            for (int o = 0; o < p.groups; ++o) {
+                const double v = scores[o];
+                before += v > own || (v == own && o < g);
+            }
+            if (g < p.groups && before >= p.top_groups)
+                for (int i = part; i < size; i += width) mine[g * size + i] = KEY::none();
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-        for (int s = 0; s < SLOTS; ++s) c[s] = sub * SLOTS + s < p.E ? mine[sub * SLOTS + s] : (Key)-HUGE_VAL;
+        for (int s = 0; s < SLOTS; ++s) c[s] = sub * SLOTS + s < p.E ? mine[sub * SLOTS + s] : KEY::none();
     }
 
     int my_id = -1;
     float my_logit = lowest();
     for (int j = 0; j < p.k; ++j) {
         Key best = c[0];
-        int at = 0;
-        float logit = l[0];
 #pragma unroll
-        for (int s = 1; s < SLOTS; ++s) {
-            const bool over = c[s] > best;
-            best = over ? c[s] : best;
-            at = over ? s : at;
-            logit = over ? l[s] : logit;
-        }
+        for (int s = 1; s < SLOTS; ++s) best = Max{}(best, c[s]);
         const Key top = over_token<LANES>(best, Max{});
-        const int e_mine = sub * SLOTS + at;
-        const int e = over_token<LANES>(best == top ? e_mine : 0x7fffffff, Min{});
-        const bool found = top > (Key)-HUGE_VAL;
-        const float of_e = over_token<LANES>(e == e_mine ? logit : lowest(), Max{});
-        if (sub == j && found) {
-            my_id = e;
-            my_logit = of_e;
-        }
+        int e_mine = 0x7fffffff;
 #pragma unroll
-        for (int s = 0; s < SLOTS; ++s)
-            if (sub * SLOTS + s == e) c[s] = (Key)-HUGE_VAL;
+        for (int s = SLOTS - 1; s >= 0; --s) e_mine = c[s] == top ? sub * SLOTS + s : e_mine;
+        const int e = over_token<LANES>(e_mine, Min{});
+        float logit = lowest();
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) {
+            const bool taken = sub * SLOTS + s == e;
+            if constexpr (WIDE) logit = taken ? l[s] : logit;
+            c[s] = taken ? KEY::none() : c[s];
+        }
+        // its logit: the key itself, or the owner's
+        if constexpr (WIDE) logit = over_token<LANES>(logit, Max{});
+        else logit = KEY::logit(top);
+        if (sub == j && top != KEY::none()) {
+            my_id = e;
+            my_logit = logit;
+        }
     }
 
     double w = 0.0;
@@ -229,24 +274,20 @@ __device__ inline int block_scan(int *v, int n, int *wave_sums)
     return before;
 }
 
-// rows and slots of the assignments of 64 tokens from `t_base` on; base[e]: place of the first of expert e
-__device__ inline void place_assignments(const RouteParams &p, int t_base, int t_end, const unsigned long long *taken, const int *base)
+// row and slot of assignment `a`, which is expert e's (-1: none) and of the token `bit` of its 64; base[e]: place of the first of
+// those 64 tokens' with expert e
+__device__ inline void place(const RouteParams &p, int a, int e, int bit, const unsigned long long *taken, const int *base)
 {
-    const int n = (min(t_end, t_base + 64) - t_base) * p.k;
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const int a = t_base * p.k + i, tok = i / p.k;
-        const int e = p.ids[a];
-        int slot = -1;
-        if (e >= 0) {
-            slot = base[e] + __popcll(taken[e] & ((1ull << tok) - 1));
-            p.rows[slot] = a;
-        }
-        p.slots[a] = slot;
+    int slot = -1;
+    if (e >= 0) {
+        slot = base[e] + __popcll(taken[e] & ((1ull << bit) - 1));
+        p.rows[slot] = a;
     }
+    p.slots[a] = slot;
 }
 
-// ONE: all tokens (at most 64) in one block, which makes the lists too.  Otherwise block b takes `span` tokens (a
-// multiple of 64) and leaves how many of them took each expert in counts[b].
+// ONE: all tokens in one block, which makes the lists too.  Otherwise block b takes `span` tokens and leaves how many of
+// them took each expert in counts[b].
 template <int LANES, int SLOTS, bool WIDE, bool ONE>
 __global__ __launch_bounds__(threads_of(SLOTS, WIDE)) void route_kernel(RouteParams p, int span)
 {
@@ -274,36 +315,59 @@ __global__ __launch_bounds__(threads_of(SLOTS, WIDE)) void route_kernel(RoutePar
         for (int e = threadIdx.x; e < p.E; e += blockDim.x) p.offsets[e] = count[e];
         if (threadIdx.x == 0) p.offsets[p.E] = all;
         // (ids are read back from memory: written by this block, before the barriers of the scan)
-        place_assignments(p, 0, p.T, taken, count);
+        for (int i = threadIdx.x; i < p.T * p.k; i += blockDim.x) place(p, i, p.ids[i], i / p.k, taken, count);
         for (int i = all + threadIdx.x; i < p.T * p.k; i += blockDim.x) p.rows[i] = -1;
     } else {
-        for (int e = threadIdx.x; e < p.E; e += blockDim.x) p.counts[(size_t)blockIdx.x * p.E + e] = count[e];
+        for (int e = threadIdx.x; e < p.Ep; e += blockDim.x) p.counts[(size_t)blockIdx.x * p.Ep + e] = e < p.E ? (uint16_t)count[e] : 0;
     }
 }
 
-__global__ __launch_bounds__(THREADS) void route_lists_kernel(RouteParams p, int span)
+// Block b makes the lists of `span` tokens (a multiple of 64): those of the blocks [b each, (b + 1) each) of the `nblocks`
+// that counted.
+__global__ __launch_bounds__(THREADS) void route_lists_kernel(RouteParams p, int span, int each, int nblocks)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     unsigned long long *taken = (unsigned long long *)smem;   // [E]
     int *base = (int *)(taken + p.E);                         // [E] all tokens' counts, then the offsets
-    int *before = base + p.E;                                 // [E] counts of the blocks before this one
+    int *before = base + p.E;                                 // [E] counts of the tokens before this block's
     int *wave_sums = before + p.E;                            // [16]
-    for (int e = threadIdx.x; e < p.E; e += blockDim.x) base[e] = before[e] = 0;
+    const int t_lo = blockIdx.x * span, t_hi = min(p.T, t_lo + span), own = blockIdx.x * each;
+    // the first 64 tokens' ids are requested ahead of the counts (at most two a thread)
+    const int n_first = (min(t_hi, t_lo + 64) - t_lo) * p.k;
+    int first[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) first[i] = (int)threadIdx.x + i * THREADS < n_first ? p.ids[t_lo * p.k + threadIdx.x + i * THREADS] : -1;
+    for (int e = threadIdx.x; e < p.E; e += blockDim.x) {
+        base[e] = before[e] = 0;
+        taken[e] = 0;
+    }
     __syncthreads();
-    // every group of threads as wide as the experts adds up a part of the blocks (whole numbers: any order)
-    const int width = min(p.E, (int)blockDim.x), parts = blockDim.x / width, part = threadIdx.x / width;
-    if (part < parts)
-        for (int e = threadIdx.x % width; e < p.E; e += width) {
-            int all = 0, ahead = 0;
-#pragma unroll 8
-            for (int b = part; b < (int)gridDim.x; b += parts) {
-                const int n = p.counts[(size_t)b * p.E + e];
-                all += n;
-                ahead += b < (int)blockIdx.x ? n : 0;
+    // a thread adds up eight experts of every `step`th block (whole numbers: any order)
+    const int octets = p.Ep / 8, step = THREADS / octets, o = threadIdx.x % octets;
+    if ((int)threadIdx.x / octets < step) {
+        int sum[8] = {}, ahead[8] = {};
+#pragma unroll 4
+        for (int b = threadIdx.x / octets; b < nblocks; b += step) {
+            const uint4 c = *(const uint4 *)(p.counts + (size_t)b * p.Ep + 8 * o);
+            const uint32_t d[4] = {c.x, c.y, c.z, c.w};
+            const bool is_ahead = b < own;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int n = (d[i >> 1] >> (16 * (i & 1))) & 0xffff;
+                sum[i] += n;
+                ahead[i] += is_ahead ? n : 0;
             }
-            atomicAdd(&base[e], all);
-            atomicAdd(&before[e], ahead);
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (8 * o + i < p.E) {
+                if (sum[i]) atomicAdd(&base[8 * o + i], sum[i]);
+                if (ahead[i]) atomicAdd(&before[8 * o + i], ahead[i]);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (first[i] >= 0) atomicOr(&taken[first[i]], 1ull << (((int)threadIdx.x + i * THREADS) / p.k));
     __syncthreads();
     const int all = block_scan(base, p.E, wave_sums);
     if (blockIdx.x == 0) {
@@ -311,9 +375,18 @@ __global__ __launch_bounds__(THREADS) void route_lists_kernel(RouteParams p, int
         if (threadIdx.x == 0) p.offsets[p.E] = all;
     }
     for (int e = threadIdx.x; e < p.E; e += blockDim.x) base[e] += before[e];
-    const int t_lo = blockIdx.x * span, t_hi = min(p.T, t_lo + span);
-    for (int t = t_lo; t < t_hi; t += 64) {
-        for (int e = threadIdx.x; e < p.E; e += blockDim.x) taken[e] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int at = (int)threadIdx.x + i * THREADS;
+        if (at < n_first) place(p, t_lo * p.k + at, first[i], at / p.k, taken, base);
+    }
+    for (int t = t_lo + 64; t < t_hi; t += 64) {
+        __syncthreads();
+        for (int e = threadIdx.x; e < p.E; e += blockDim.x) {
+            base[e] += __popcll(taken[e]);
+            taken[e] = 0;
+        }
         __syncthreads();
         const int n = (min(t_hi, t + 64) - t) * p.k;
         for (int i = threadIdx.x; i < n; i += blockDim.x) {
@@ -321,29 +394,33 @@ __global__ __launch_bounds__(THREADS) void route_lists_kernel(RouteParams p, int
             if (e >= 0) atomicOr(&taken[e], 1ull << (i / p.k));
         }
         __syncthreads();
-        place_assignments(p, t, t_hi, taken, base);
-        __syncthreads();
-        for (int e = threadIdx.x; e < p.E; e += blockDim.x) base[e] += __popcll(taken[e]);
+        for (int i = threadIdx.x; i < n; i += blockDim.x) place(p, t * p.k + i, p.ids[t * p.k + i], i / p.k, taken, base);
     }
     // places behind the last assignment
     for (long i = (long)t_lo * p.k + threadIdx.x; i < (long)t_hi * p.k; i += blockDim.x)
         if (i >= all) p.rows[i] = -1;
 }
 
-// tokens of a block of the counting launch: whole groups of 64, in at most MAX_LIST_BLOCKS blocks
-int route_span(int T) { return 64 * ((T + 64 * MAX_LIST_BLOCKS - 1) / (64 * MAX_LIST_BLOCKS)); }
+// tokens of a block of the counting launch: a power of two from 4 on up to 64, then whole groups of 64 (counts fit 16 bits)
+int route_span(int T)
+{
+    int span = 4;
+    while (span < 64 && (T + span - 1) / span > MAX_BLOCKS) span *= 2;
+    return span < 64 ? span : 64 * ((T + 64 * MAX_BLOCKS - 1) / (64 * MAX_BLOCKS));
+}
 
 template <int LANES, int SLOTS>
 int launch_lanes(const RouteParams &p, bool wide, hipStream_t st)
 {
     constexpr int TPW = 64 / LANES;
-    const bool one = p.T <= 64;
+    const bool one = p.T <= ONE_LAUNCH;
+    const int span = one ? ONE_LAUNCH : route_span(p.T), blocks = one ? 1 : (p.T + span - 1) / span;
     // a wave for every TPW tokens, as many as a block holds; the lists want a few for the experts
     const size_t wave_cells = p.groups > 1 ? (size_t)TPW * (p.E + p.groups) * sizeof(double) : 0;
-    const int most = threads_of(SLOTS, wide) / 64;
-    int waves = one ? std::min(most, std::max((p.T + TPW - 1) / TPW, (p.E + 63) / 64)) : most;
+    int waves = (std::min(one ? std::max(p.T, 1) : span, 64) + TPW - 1) / TPW;
+    if (one) waves = std::max(waves, std::min(4, (p.E + 63) / 64));
+    waves = std::min(waves, threads_of(SLOTS, wide) / 64);
     if (wave_cells) waves = std::min(waves, (int)(LDS_CELLS / wave_cells));
-    const int span = one ? 64 : route_span(p.T), blocks = one ? 1 : (p.T + span - 1) / span;
     const size_t lds = (size_t)p.E * 8 + (size_t)(p.E + (p.E & 1)) * 4 + 64 + waves * wave_cells;
     auto go = [&](auto kernel) {
         if (lds > 48 * 1024)
@@ -351,9 +428,13 @@ int launch_lanes(const RouteParams &p, bool wide, hipStream_t st)
         hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64 * waves), lds, st, p, span);
         return (int)hipGetLastError();
     };
-    if (one) return wide ? go(route_kernel<LANES, SLOTS, true, true>) : go(route_kernel<LANES, SLOTS, false, true>);
+    if (one) {
+        if constexpr (LANES == 64) return wide ? go(route_kernel<LANES, SLOTS, true, true>) : go(route_kernel<LANES, SLOTS, false, true>);
+        return (int)hipErrorInvalidValue;
+    }
     if (int e = wide ? go(route_kernel<LANES, SLOTS, true, false>) : go(route_kernel<LANES, SLOTS, false, false>)) return e;
-    hipLaunchKernelGGL(route_lists_kernel, dim3(blocks), dim3(THREADS), (size_t)p.E * 16 + 64, st, p, span);
+    const int list_span = std::max(span, 64), lists = (p.T + list_span - 1) / list_span;
+    hipLaunchKernelGGL(route_lists_kernel, dim3(lists), dim3(THREADS), (size_t)p.E * 16 + 64, st, p, list_span, list_span / span, blocks);
     return (int)hipGetLastError();
 }
 
@@ -361,20 +442,25 @@ int launch_lanes(const RouteParams &p, bool wide, hipStream_t st)
 
 size_t route_workspace_bytes(int T, int E)
 {
-    if (T <= 64) return 0;
+    if (T <= ONE_LAUNCH) return 0;
     const int span = route_span(T);
-    return (size_t)((T + span - 1) / span) * E * sizeof(int32_t);
+    return (size_t)((T + span - 1) / span) * round_up(E, 8) * sizeof(uint16_t);
 }
 
-int launch_route(const RouteParams &p, hipStream_t st)
+int launch_route(const RouteParams &p0, hipStream_t st)
 {
+    RouteParams p = p0;
+    p.Ep = round_up(p.E, 8);
     // 64-bit keys wherever the order of the choice is not that of the logits
     const bool wide = p.bias || (p.groups > 1 && p.group_top2);
-    if (p.E <= 256 && p.k <= 16) {
+    // four tokens a wave where a wave for every token would be more than the chip runs at once
+    if (p.T > 16 * cu_count() && p.E <= 256 && p.k <= 16) {
         if (p.E <= 64) return launch_lanes<16, 4>(p, wide, st);
         if (p.E <= 128) return launch_lanes<16, 8>(p, wide, st);
         return launch_lanes<16, 16>(p, wide, st);
     }
+    if (p.E <= 64) return launch_lanes<64, 1>(p, wide, st);
+    if (p.E <= 128) return launch_lanes<64, 2>(p, wide, st);
     if (p.E <= 256) return launch_lanes<64, 4>(p, wide, st);
     return launch_lanes<64, 16>(p, wide, st);
 }

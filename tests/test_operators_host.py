@@ -59,7 +59,7 @@ def route(ptr=FAKE, ws=FAKE, nbytes=1 << 30, logits=FAKE, bias=None, **kw):
     dict(T=-1), dict(E=0), dict(top_k=0), dict(top_k=17), dict(groups=0), dict(groups=3), dict(top_groups=0), dict(top_groups=2),
     dict(logits_stride=15), dict(score=2), dict(score=-1), dict(group_score=2), dict(logits_fp16=2), dict(renormalize=3),
     dict(ptr=None), dict(ptr=FAKE + 2), dict(logits=None), dict(logits=FAKE + 2), dict(logits=FAKE + 1, logits_fp16=1), dict(bias=FAKE + 1),
-    dict(ws=None), dict(ws=FAKE + 1),
+    dict(ws=None), dict(ws=FAKE + 8),
 ])
 def test_bad_routes_are_refused(kw):
     assert route(**kw) == EINVAL
@@ -70,17 +70,17 @@ def test_routes_beyond_the_limits_are_refused():
     assert route(E=64, logits_stride=64, top_k=33) == EUNSUPPORTED
     assert route(E=130, logits_stride=130, groups=65, top_groups=1) == EUNSUPPORTED
     assert route(T=(1 << 24) + 1) == EUNSUPPORTED
-    assert route(nbytes=2 * 16 * 4 - 1) == EWORKSPACE   # 100 tokens: two blocks of 64
+    assert route(nbytes=25 * 16 * 2 - 1) == EWORKSPACE   # 100 tokens: 25 blocks of four
     L = mx.lib()
     assert L.mixllm_route_experts(None, *[FAKE] * 9, 0, None) == EINVAL
 
 
 def test_route_workspace():
     need = lambda T, E: mx.lib().mixllm_route_workspace(C.byref(binding._RouteDesc(T, E, 1, 0, E, 0, 1, 1, 0, 0, 1.0)))
-    assert need(0, 16) == need(64, 16) == 0
-    assert need(65, 16) == 2 * 16 * 4 and need(16384, 16) == 256 * 16 * 4
-    assert need(16385, 10) == 129 * 10 * 4               # 128 tokens a block from there on
-    assert need(1 << 24, 1024) == 256 * 1024 * 4
+    assert need(0, 16) == need(16, 16) == 0
+    assert need(17, 16) == 5 * 16 * 2 and need(1025, 16) == 129 * 16 * 2 and need(16384, 16) == 256 * 16 * 2
+    assert need(16385, 10) == 129 * 16 * 2               # 128 tokens a block from there on
+    assert need(1 << 24, 1023) == 256 * 1024 * 2
     assert need(10, 1025) == 0                            # (refused)
 
 
