@@ -107,6 +107,37 @@ def check_hand_issued_loads(asm_text: str, name: str) -> None:
         raise RuntimeError("registers of hand-issued loads are used before their wait:\n  " + "\n  ".join(bad[:10]))
 
 
+def check_scalar_bases(asm_text: str, name: str) -> None:
+    """A scalar register written by a vector instruction - a lane read, or the reload of a scalar spilled to a vector
+    register's lanes - may be read by a vector-memory instruction only 5 wait states later.  The compiler fills them in
+    in front of its own loads, but not in front of one inside an asm statement, whose base is then a stale address."""
+    def scalars(text):
+        out = set()
+        for a, b in re.findall(r"\bs\[(\d+):(\d+)\]", text):
+            out |= set(range(int(a), int(b) + 1))
+        return out | {int(a) for a in re.findall(r"\bs(\d+)\b", text)}
+    written, now, in_asm, bad = {}, 0, False, []
+    for i, line in enumerate(asm_text.split("\n"), 1):
+        t = line.strip()
+        if t.startswith((";;#ASMSTART", ";;#ASMEND")):
+            in_asm = t.startswith(";;#ASMSTART")
+            continue
+        if not t or t[0] in ";." or t.endswith(":"):
+            continue
+        if in_asm and t.startswith("global_load_"):
+            close = [r for r in scalars(t) if now - written.get(r, -9) < 5]
+            if close:
+                bad.append(f"{name}.s:{i}: `{t[:70]}` reads s{sorted(close)}, written by a vector instruction less than 5 wait states before")
+        now += 1 + (int(t.split()[1], 0) if t.startswith("s_nop") else 0)
+        if t.startswith(("v_readlane", "v_readfirstlane")):
+            written.update(dict.fromkeys(scalars(t.split(",")[0]), now))
+        elif t.startswith("s_"):
+            for r in scalars(t.split(",")[0]):
+                written.pop(r, None)
+    if bad:
+        raise RuntimeError("hand-issued loads read scalar registers too early:\n  " + "\n  ".join(bad[:10]))
+
+
 # Sources whose kernels pass the path-following scan of asm_scan.py (every path through the control-flow
 # graph, loop back edges included).  The others issue or await some loads under conditions the scan cannot
 # relate to each other (the same uniform test before the load and before its wait), which it reports as
@@ -206,6 +237,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
         try:
             text = open(a).read()
             check_hand_issued_loads(text, src)
+            check_scalar_bases(text, src)
             if src in FULL_SCAN:
                 asm_scan.check_hand_issued_loads(text, src)
             if src in RING_COPY_LIMIT:

@@ -23,6 +23,21 @@ static __device__ inline void load_lds16(uint32_t lds_base, uint32_t voff, const
 {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(voff), "s"(sbase) : "memory", "m0");
 }
+// The same where the base may have been put into its registers by a vector instruction just before (a lane read, or the
+// reload of a spilled scalar): a memory instruction may read such a register only five wait states later, and the
+// compiler, which fills them in for its own loads, does not look into an asm statement.  The build checks the
+// distance for every hand-issued load.
+static __device__ inline void load_lds16_spaced(uint32_t lds_base, uint32_t voff, const void *sbase)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(voff), "s"(sbase) : "memory", "m0");
+}
+// a scalar address that a vector instruction has just written, ready for a hand-issued load
+template <typename T>
+static __device__ inline T *spaced(T *p)
+{
+    asm volatile("s_nop 4" : "+s"(p));
+    return p;
+}
 template <int OFF>
 static __device__ inline void load_reg16(v4i &dst, uint32_t voff, const void *sbase)
 {

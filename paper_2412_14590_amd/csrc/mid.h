@@ -133,7 +133,7 @@ __device__ inline void mid_block(const LinearParams &p, const MidArgs &a, uint8_
     auto load_a = [&](int q, int buf) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
-            load_lds16(lds_base + buf * STAGE + a_lds[i], a_voff[i], p.xq + (size_t)min(4 * q + a_group[i], ng - 1) * G);
+            load_lds16_spaced(lds_base + buf * STAGE + a_lds[i], a_voff[i], p.xq + (size_t)min(4 * q + a_group[i], ng - 1) * G);
     };
     // fragment reads: token row 16 mt + c, 16-byte chunk ks (k 0..63 of the group) and 4 + ks
     const int sw = (c >> 1) & 7;

@@ -187,3 +187,23 @@ def test_python_calls_refuse_wrong_operands(monkeypatch):
     refused(lambda: mx.pack_experts([]), "experts of one size")
     other = binding.PackedLayer(128, 64, 8, 128, L.w8, L.w4, L.s8, L.s4, L.z4, L.perm)
     refused(lambda: mx.pack_experts([L, other]), "experts of one size")
+
+
+LOAD = "\t;;#ASMSTART\n\tglobal_load_dwordx4 v[0:3], v4, s[6:7] offset:0\n\t;;#ASMEND\n"
+
+
+@pytest.mark.parametrize("between,ok", [
+    ("", False), ("\tv_add_u32_e32 v9, v8, v7\n" * 4, False), ("\tv_add_u32_e32 v9, v8, v7\n" * 5, True), ("\ts_nop 4\n", True), ("\ts_nop 3\n", False),
+    ("\ts_add_u32 s6, s6, 16\n\ts_addc_u32 s7, s7, 0\n", True),       # rewritten by the scalar unit
+    ("\ts_add_u32 s6, s6, 16\n", False),                              # ... half of it
+    (".LBB0_1:\n\ts_branch .LBB0_2\n", False),
+])
+def test_the_build_checks_the_distance_of_a_scalar_base(between, ok):
+    from paper_2412_14590_amd import build
+    text = "\tv_readlane_b32 s6, v40, s3\n\tv_readfirstlane_b32 s7, v41\n" + between + LOAD
+    if ok:
+        build.check_scalar_bases(text, "x")
+    else:
+        with pytest.raises(RuntimeError):
+            build.check_scalar_bases(text, "x")
+    build.check_scalar_bases(text.replace("s6, v40", "s8, v40").replace("s7, v41", "s9, v41"), "x")
