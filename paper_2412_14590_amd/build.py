@@ -17,7 +17,7 @@ PROBE_LIB = os.path.join(HERE, "libmixllm_probe.so")
 CALLS = os.path.join(HERE, "_calls.so")   # the native part of the Python binding (binding.py)
 SOURCES = ["api.hip", "quant_act.hip", "quant_weights.hip", "linear_generic.hip",
            "linear_decode.hip", "linear_decode_split.hip", "linear_mid.hip", "linear_prefill.hip", "salience.hip",
-           "epilogue_decode_split.hip", "epilogue_mid.hip", "epilogue_tiled.hip", "route.hip", "experts.hip"]
+           "epilogue_decode_split.hip", "epilogue_mid.hip", "epilogue_tiled.hip", "route.hip", "experts.hip", "experts_stream.hip"]
 HEADERS = [os.path.join(CSRC, h) for h in ("internal.h", "async_loads.h", "epilogue.h", "tiled.h", "decode_split.h", "mid.h", "experts.h")] + [os.path.join(INCLUDE, "mixllm.h")]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -40,7 +40,8 @@ _TILED = lambda n: "linear_prefill_kernel" in n or "linear_slices_kernel" in n
 _SPLIT = lambda n: "linear_decode_split_kernel" in n
 _MID = lambda n: "linear_mid_kernel" in n
 NO_SPILL = {"linear_prefill.hip": _TILED, "epilogue_tiled.hip": _TILED, "linear_decode_split.hip": _SPLIT, "epilogue_decode_split.hip": _SPLIT,
-            "linear_mid.hip": _MID, "epilogue_mid.hip": _MID, "experts.hip": lambda n: "experts_tiled_kernel" in n}
+            "linear_mid.hip": _MID, "epilogue_mid.hip": _MID, "experts.hip": lambda n: "experts_tiled_kernel" in n,
+            "experts_stream.hip": lambda n: "experts_stream_kernel" in n}
 
 
 def _check_no_scratch(src: str, compile_log: str) -> None:
@@ -142,7 +143,7 @@ def check_scalar_bases(asm_text: str, name: str) -> None:
 # graph, loop back edges included).  The others issue or await some loads under conditions the scan cannot
 # relate to each other (the same uniform test before the load and before its wait), which it reports as
 # paths without a wait; they get the straight-line scan above and the tripwire below.
-FULL_SCAN = {"linear_prefill.hip", "epilogue_tiled.hip", "experts.hip"}
+FULL_SCAN = {"linear_prefill.hip", "epilogue_tiled.hip", "experts.hip", "experts_stream.hip"}
 # Kernels that keep a ring of hand-issued loads in flight around a rolled loop: registers of the ring must
 # stay where they are.  Where the loop nest makes the compiler rotate them (seen with the chunk loop of
 # the evenly split decode kernel nested in a loop over activation windows: 80 to 220 copies, at the loop

@@ -19,10 +19,35 @@ static __device__ inline int wave_scan(int v)
 static __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // first place and rows of expert e, clamped to the places there are
-static __device__ inline void expert_rows(const ExpertsArgs &a, int e, int &first, int &count)
+static __device__ inline void clamp_rows(const ExpertsArgs &a, int lo, int hi, int &first, int &count)
 {
-    first = min(max(a.offsets[e], 0), a.places);
-    count = max(min(a.offsets[e + 1], a.places) - first, 0);
+    first = min(max(lo, 0), a.places);
+    count = max(min(hi, a.places) - first, 0);
+}
+static __device__ inline void expert_rows(const ExpertsArgs &a, int e, int &first, int &count) { clamp_rows(a, a.offsets[e], a.offsets[e + 1], first, count); }
+
+// The same and its entry of the table for an expert that is the same for the whole wave: by scalar loads, which come back
+// past the hand-issued vector loads in flight (nothing writes either array while the kernels of the experts run).
+template <typename T>
+using constant_t = const __attribute__((address_space(4))) T;
+static __device__ inline void expert_rows_uniform(const ExpertsArgs &a, int e, int &first, int &count)
+{
+    constant_t<int32_t> *o = (constant_t<int32_t> *)a.offsets;
+    e = uniform(e);
+    clamp_rows(a, o[e], o[e + 1], first, count);
+}
+static __device__ inline ExpertEntry expert_entry(const ExpertsArgs &a, int e)
+{
+    constant_t<ExpertEntry> *t = (constant_t<ExpertEntry> *)a.table + uniform(e);
+    return ExpertEntry{t->w4, t->w8, t->s4, t->s8, t->z4, t->perm, t->n8, t->n4, t->ntiles8, t->ntiles4};
+}
+
+// Row `m` of an expert's (or the batch's) rows as a row of the activations: itself, or through the route's list
+template <bool ROWS>
+static __device__ inline int token_row(const LinearParams &p, int m)
+{
+    if constexpr (ROWS) return p.rows ? min((int)((unsigned)p.rows[m] / (unsigned)p.rows_per_token), p.tokens - 1) : m;
+    return m;
 }
 
 }  // namespace mixllm

@@ -23,16 +23,17 @@ __global__ void experts_table_kernel(ExpertEntry *table, TableChunk chunk, int f
     if ((int)threadIdx.x < n) table[first + threadIdx.x] = chunk.entry[threadIdx.x];
 }
 
-// Logical tiles: those of the 4-bit parts of all experts, then those of the 8-bit parts; in a part expert by expert, the
-// row tiles of a column of channels next to each other.  As in the tiled kernel every XCD (blocks are dealt to them round
-// robin) takes a contiguous range of the 4-bit tiles, so that the blocks that share an expert's weights and rows share
-// an L2, and ends on its range of the cheaper 8-bit ones.
-template <typename C, bool ACT_PT, bool W8PC>
-__global__ __launch_bounds__(C::THREADS, 2) void experts_tiled_kernel(LinearParams p, ExpertsArgs a)
+// The tile of this block, and p made that of its expert.  Logical tiles: those of the 4-bit parts of all experts, then those
+// of the 8-bit parts; in a part expert by expert, the row tiles of a column of channels next to each other.  As in the tiled
+// kernel every XCD (blocks are dealt to them round robin) takes a contiguous range of the 4-bit tiles, so that the blocks that
+// share an expert's weights and rows share an L2, and ends on its range of the cheaper 8-bit ones.
+struct TileOf {
+    bool none, part8;
+    int bm, bn;
+};
+template <int BM4, int BM8, int T16, bool ACT_PT>
+static __device__ __forceinline__ TileOf find_tile(LinearParams &p, const ExpertsArgs &a)
 {
-    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    using C8 = typename C::Half;
-    constexpr int T16 = C::BN / TILE_N;
     const int lane = threadIdx.x & 63;
     // tiles of expert e in either part
     auto tiles_of = [&](int e, int &t4, int &t8) {
@@ -40,8 +41,8 @@ __global__ __launch_bounds__(C::THREADS, 2) void experts_tiled_kernel(LinearPara
         if (e < a.E) {
             int first, count;
             expert_rows(a, e, first, count);
-            t4 = (count + C::BM - 1) / C::BM * ((a.table[e].ntiles4 + T16 - 1) / T16);
-            t8 = (count + C8::BM - 1) / C8::BM * ((a.table[e].ntiles8 + T16 - 1) / T16);
+            t4 = (count + BM4 - 1) / BM4 * ((a.table[e].ntiles4 + T16 - 1) / T16);
+            t8 = (count + BM8 - 1) / BM8 * ((a.table[e].ntiles8 + T16 - 1) / T16);
         }
     };
     int total4 = 0, total8 = 0;
@@ -55,14 +56,16 @@ __global__ __launch_bounds__(C::THREADS, 2) void experts_tiled_kernel(LinearPara
     total8 = uniform(__shfl(wave_scan(total8), 63));
     const int per4 = (total4 + 7) / 8, per8 = (total8 + 7) / 8;
     const int xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
-    const bool part8 = i >= per4;
-    const int L = part8 ? xcd * per8 + (i - per4) : xcd * per4 + i;
-    if (part8 ? (i - per4 >= per8 || L >= total8) : L >= total4) return;
+    TileOf t;
+    t.part8 = i >= per4;
+    const int L = t.part8 ? xcd * per8 + (i - per4) : xcd * per4 + i;
+    t.none = t.part8 ? (i - per4 >= per8 || L >= total8) : L >= total4;
+    if (t.none) return t;
     int e = 0, before = 0;
     for (int e0 = 0, sum = 0; e0 < a.E; e0 += 64) {
         int t4, t8;
         tiles_of(e0 + lane, t4, t8);
-        const int own = part8 ? t8 : t4, upto = sum + wave_scan(own);
+        const int own = t.part8 ? t8 : t4, upto = sum + wave_scan(own);
         const unsigned long long here = __ballot(own > 0 && L >= upto - own && L < upto);
         if (here) {
             const int l = __ffsll(here) - 1;
@@ -72,9 +75,9 @@ __global__ __launch_bounds__(C::THREADS, 2) void experts_tiled_kernel(LinearPara
         }
         sum = uniform(__shfl(upto, 63));
     }
-    const ExpertEntry &x = a.table[e];
+    const ExpertEntry x = expert_entry(a, e);
     int first, count;
-    expert_rows(a, e, first, count);
+    expert_rows_uniform(a, e, first, count);
     p.w4 = x.w4;
     p.w8 = x.w8;
     p.s4 = x.s4;
@@ -93,17 +96,29 @@ __global__ __launch_bounds__(C::THREADS, 2) void experts_tiled_kernel(LinearPara
     }
     p.y += (size_t)first * (p.ep.gated ? p.N / 2 : p.N);
     if (p.ep.bias) p.ep.bias += (size_t)e * p.N;
-    const int BM = part8 ? C8::BM : C::BM;
-    const int nbm = (count + BM - 1) / BM, r = L - before, bn = r / nbm, bm = r - bn * nbm;
+    const int BM = t.part8 ? BM8 : BM4, nbm = (count + BM - 1) / BM, r = L - before;
+    t.bn = uniform(r / nbm);
+    t.bm = r - t.bn * nbm;
+    return t;
+}
+
+template <typename C, bool ACT_PT, bool W8PC>
+__global__ __launch_bounds__(C::THREADS, 2) void experts_tiled_kernel(LinearParams p, ExpertsArgs a)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    using C8 = typename C::Half;
+    constexpr int T16 = C::BN / TILE_N;
+    const TileOf t = find_tile<C::BM, C8::BM, T16, ACT_PT>(p, a);
+    if (t.none) return;
     uint8_t *lds_a = smem;
     float *lds_sa = (float *)(smem + NSTAGE * C::A_STAGE);
-    if (part8) {
+    if (t.part8) {
         if constexpr (W8PC && ACT_PT)
-            prefill_block_w8_channel_scale<C8, ACT_PT, 0, true, true>(p, bm * C8::BM, bn * T16, 0, p.ng, 0, lds_a, lds_sa, smem);
+            prefill_block_w8_channel_scale<C8, ACT_PT, 0, true, true>(p, t.bm * C8::BM, t.bn * T16, 0, p.ng, 0, lds_a, lds_sa, smem);
         else
-            prefill_block<C8, 0, ACT_PT, true, !W8PC, true, true, true>(p, bm * C8::BM, bn * T16, 0, p.ng, 0, lds_a, lds_sa, smem);
+            prefill_block<C8, 0, ACT_PT, true, !W8PC, true, true, true>(p, t.bm * C8::BM, t.bn * T16, 0, p.ng, 0, lds_a, lds_sa, smem);
     } else
-        prefill_block<C, 0, ACT_PT, false, false, true, true, true>(p, bm * C::BM, bn * T16, 0, p.ng, 0, lds_a, lds_sa, smem);
+        prefill_block<C, 0, ACT_PT, false, false, true, true, true>(p, t.bm * C::BM, t.bn * T16, 0, p.ng, 0, lds_a, lds_sa, smem);
 }
 
 template <typename C>
@@ -183,6 +198,7 @@ int launch_experts_linear(const LinearParams &p, const ExpertsArgs &a, hipStream
 {
     if (!experts_cover(p)) return (int)hipErrorInvalidValue;
     if (a.places == 0) return (int)hipSuccess;
+    if (p.x) return launch_experts_stream(p, a, st);
     const long mean = a.places / a.E;   // rows of an expert
     if (mean > 64 && p.act_per_token) return launch_experts_shape<Shape<1, 4, 4, MIXLLM_PREFILL_WD_LARGE>>(p, a, st);
     if (mean > 24) return launch_experts_shape<Shape<1, 4, 2, MIXLLM_PREFILL_WD_SMALL>>(p, a, st);

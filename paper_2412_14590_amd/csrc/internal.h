@@ -299,6 +299,9 @@ struct ExpertsArgs {
 };
 int launch_experts_table(int E, int N, const mixllm_expert *experts, ExpertEntry *table, hipStream_t st);
 bool experts_cover(const LinearParams &p);
+// kernel for a token or a few, from fp16 activations (p.x) that it quantizes itself (experts_stream.hip)
+bool experts_stream_covers(const LinearParams &p, const ExpertsArgs &a);
+int launch_experts_stream(const LinearParams &p, const ExpertsArgs &a, hipStream_t st);
 // p: M = rows of xq, rows / rows_per_token as the kernels read them (null: a row per place), the rest but the layer's own
 int launch_experts_linear(const LinearParams &p, const ExpertsArgs &a, hipStream_t st);
 int launch_experts_combine(int T, int k, int N, int places, const void *y, const float *weights, const int32_t *slots, const void *residual,

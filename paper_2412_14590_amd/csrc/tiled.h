@@ -44,6 +44,7 @@
 
 #include "async_loads.h"
 #include "epilogue.h"
+#include "experts.h"
 #include "internal.h"
 
 namespace mixllm {
@@ -305,14 +306,6 @@ static __device__ __forceinline__ void combine_slices(const LinearParams &p, int
                 if (m0 + row + i < p.M && ch >= 0) p.y[(size_t)(m0 + row + i) * p.N + ch] = (half_t)result(v[i], row + i);
         }
     }
-}
-
-// Row `m` of an expert's (or the batch's) rows as a row of the activations: itself, or through the route's list
-template <bool ROWS>
-static __device__ inline int token_row(const LinearParams &p, int m)
-{
-    if constexpr (ROWS) return p.rows ? min((int)((unsigned)p.rows[m] / (unsigned)p.rows_per_token), p.tokens - 1) : m;
-    return m;
 }
 
 // ASYNC: packed weights and metadata are fetched with the hand-issued loads above.  Only valid in a
