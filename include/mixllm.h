@@ -356,7 +356,8 @@ int mixllm_experts_table(const mixllm_desc *d, int32_t E, const mixllm_expert *e
 /*
  * The products of the experts over the rows that a route gave them: for every expert e and place p in
  * [offsets[e], offsets[e + 1]) the linear of expert e with its epilogue, from one row of activations to row p of y.
- *   d             M = rows of xq; K, N, group, act_group, w8_group; n8 is not read
+ *   d             M = rows of xq; K, N, group, act_group, w8_group; n8: the largest of the experts' (or N: any number
+ *                 at least as large is right, and takes longer; with a smaller one rows of y stay unwritten)
  *   gather        top_k > 0: xq has a row per token, place p reads that of token rows[p] / top_k, and there are
  *                 M top_k places (the first product); 0: xq has a row per place, there are M places and `rows` is not
  *                 read (the second product)

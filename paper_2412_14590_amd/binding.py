@@ -395,6 +395,7 @@ class PackedExperts:
     w8_group: int
     layers: list            # of PackedLayer: what the table points to
     table: torch.Tensor
+    n8: int                 # the most 8-bit channels of any of them
 
     @property
     def E(self) -> int:
@@ -412,7 +413,7 @@ def pack_experts(layers) -> PackedExperts:
     table = torch.empty(int(lib().mixllm_experts_table_bytes(len(layers))), dtype=torch.uint8, device=first.perm.device)
     d = first.desc()
     _check(lib().mixllm_experts_table(C.byref(d), len(layers), entries, _ptr(table), _stream()), "mixllm_experts_table")
-    return PackedExperts(first.K, first.N, first.w8_group, layers, table)
+    return PackedExperts(first.K, first.N, first.w8_group, layers, table, max(L.n8 for L in layers))
 
 
 def experts_linear(xq: torch.Tensor, xs: torch.Tensor, L: PackedExperts, route: Route, bias=None, activation=None, gated: bool = False,
@@ -420,14 +421,14 @@ def experts_linear(xq: torch.Tensor, xs: torch.Tensor, L: PackedExperts, route: 
     """The linears of the experts over the rows routed to them: y [T * top_k, N] (gated [.., N/2]), one row per assignment in the
     route's order; rows behind the last assignment are left as they were.  gather: xq has a row per token; otherwise one per
     assignment, in the route's order.  bias fp16 [E,N]; activation and gated as in mixed_linear_epilogue."""
-    return _result(_calls().experts_linear(xq, xs, L.K, L.N, L.w8_group, L.E, L.table, route.offsets, route.rows, route.slots, gather, bias,
+    return _result(_calls().experts_linear(xq, xs, L.K, L.N, L.w8_group, L.E, L.table, L.n8, route.offsets, route.rows, route.slots, gather, bias,
                                            _named(ACTIVATIONS, activation, "activation"), gated, out, _stream()), "mixllm_experts_linear")
 
 
 def experts_linear_fp16(x: torch.Tensor, L: PackedExperts, route: Route, bias=None, activation=None, gated: bool = False,
                         gather: bool = True, act_group=None, out=None, workspace=None) -> torch.Tensor:
     """experts_linear from fp16 activations x [T,K] (gather) or [T * top_k, K]: quantizer and products."""
-    return _result(_calls().experts_linear_fp16(x, L.K, L.N, L.w8_group, L.E, L.table, route.offsets, route.rows, route.slots, gather,
+    return _result(_calls().experts_linear_fp16(x, L.K, L.N, L.w8_group, L.E, L.table, L.n8, route.offsets, route.rows, route.slots, gather,
                                                 L.K if act_group is None else act_group, bias,
                                                 _named(ACTIVATIONS, activation, "activation"), gated, out, workspace, _stream()),
                    "mixllm_experts_linear_fp16")

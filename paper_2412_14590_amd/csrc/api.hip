@@ -644,18 +644,10 @@ static size_t experts_scratch(const mixllm_desc &d, size_t &xq_bytes)
     return xq_bytes + round_up_sz(s.xscale_bytes, 256);
 }
 
-static int check_experts_desc(const mixllm_desc *d)
-{
-    if (!d) return MIXLLM_EINVAL;
-    mixllm_desc own = *d;
-    own.n8 = 0;   // (not read: every expert has its own)
-    return check_desc(&own);
-}
-
 size_t mixllm_experts_workspace(const mixllm_desc *d)
 {
     size_t xq_bytes;
-    return check_experts_desc(d) == MIXLLM_OK ? experts_scratch(*d, xq_bytes) : 0;
+    return check_desc(d) == MIXLLM_OK ? experts_scratch(*d, xq_bytes) : 0;
 }
 
 // Exactly one of (xq, xscale) and x is given.
@@ -663,9 +655,8 @@ static int experts_common(const mixllm_desc *d0, int32_t E, const void *table, c
                           const int32_t *offsets, const int32_t *rows, int32_t gather, const mixllm_epilogue *epilogue, void *y,
                           void *workspace, size_t workspace_bytes, hipStream_t st)
 {
-    if (int rc = check_experts_desc(d0)) return rc;
-    mixllm_desc d = *d0;
-    d.n8 = 0;
+    if (int rc = check_desc(d0)) return rc;
+    const mixllm_desc &d = *d0;
     if (E <= 0 || gather < 0 || gather > MIXLLM_MAX_TOP_K) return MIXLLM_EINVAL;
     if (E > MIXLLM_MAX_EXPERTS) return MIXLLM_EUNSUPPORTED;
     LinearParams p = make_params(d, xq, xscale, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
@@ -689,7 +680,7 @@ static int experts_common(const mixllm_desc *d0, int32_t E, const void *table, c
     p.rows = gather ? rows : nullptr;
     p.rows_per_token = std::max(gather, 1);
     p.tokens = d.M;
-    ExpertsArgs a{(const ExpertEntry *)table, offsets, E, (int)places};
+    ExpertsArgs a{(const ExpertEntry *)table, offsets, E, (int)places, d.n8};
     if (x && experts_stream_covers(p, a)) p.x = (const half_t *)x;   // one kernel
     else if (x)
         if (int rc = hip_status(launch_quantize_activations(d, x, (int8_t *)p.xq, (void *)p.xscale, st))) return rc;

@@ -5,16 +5,17 @@
 
 namespace mixllm {
 
-// inclusive sum over the lanes of a wave (all active)
+// inclusive sum over the lanes of a wave (all active), inside rows of 16 lanes, then over the rows: six additions
+template <int CTRL, int ROWS>
+static __device__ inline int add_dpp(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
 static __device__ inline int wave_scan(int v)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
-    return v;
+    v = add_dpp<0x111, 0xf>(v);   // row_shr:1, 2, 4, 8
+    v = add_dpp<0x112, 0xf>(v);
+    v = add_dpp<0x114, 0xf>(v);
+    v = add_dpp<0x118, 0xf>(v);
+    v = add_dpp<0x142, 0xa>(v);   // row_bcast:15 into rows 1 and 3
+    return add_dpp<0x143, 0xc>(v);   // row_bcast:31 into rows 2 and 3
 }
 static __device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 

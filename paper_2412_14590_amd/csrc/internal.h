@@ -296,6 +296,7 @@ struct ExpertsArgs {
     const int32_t *offsets;   // [E + 1]
     int E;
     int places;               // rows of y at most
+    int n8;                   // 8-bit channels of an expert at most
 };
 int launch_experts_table(int E, int N, const mixllm_expert *experts, ExpertEntry *table, hipStream_t st);
 bool experts_cover(const LinearParams &p);

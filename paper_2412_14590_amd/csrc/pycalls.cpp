@@ -424,14 +424,14 @@ void list_of(const at::Tensor &t, int64_t n, const char *what)
     if (!t.defined() || t.scalar_type() != at::kInt || t.numel() != n) throw Refused{what};
 }
 
-// K, N, w8_group, E, table of the experts; offsets, rows, slots of the route; gather
+// K, N, w8_group, E, table, n8 of the experts; offsets, rows, slots of the route; gather
 struct Experts {
-    int32_t K, N, w8_group, E;
+    int32_t K, N, w8_group, E, n8;
     at::Tensor table, offsets, rows, slots;
     bool gather;
     explicit Experts(PyObject *const *a)
-        : K(number(a[0])), N(number(a[1])), w8_group(number(a[2])), E(number(a[3])), table(tensor(a[4])), offsets(tensor(a[5])), rows(tensor(a[6])),
-          slots(tensor(a[7])), gather(truth(a[8]))
+        : K(number(a[0])), N(number(a[1])), w8_group(number(a[2])), E(number(a[3])), n8(number(a[5])), table(tensor(a[4])), offsets(tensor(a[6])),
+          rows(tensor(a[7])), slots(tensor(a[8])), gather(truth(a[9]))
     {
         list_of(offsets, (int64_t)E + 1, "the route and the layer agree in their experts");
         if (!slots.defined() || slots.dim() != 2 || slots.scalar_type() != at::kInt) throw Refused{"slots: int32, tokens x top_k"};
@@ -450,12 +450,12 @@ struct Experts {
 template <bool FP16>
 PyObject *py_experts_linear(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    return run(n, FP16 ? 17 : 16, [&]() -> PyObject * {
+    return run(n, FP16 ? 18 : 17, [&]() -> PyObject * {
         const at::Tensor x = tensor(a[0]), xs = FP16 ? at::Tensor() : tensor(a[1]);
         const Experts L(a + (FP16 ? 1 : 2));
-        PyObject *const *rest = a + 11;   // bias, activation, gated, out, (workspace,) stream
+        PyObject *const *rest = a + 12;   // bias, activation, gated, out, (workspace,) stream
         if (FP16) half_matrix(x);
-        const int32_t act_group = FP16 ? number(a[10]) : codes_and_scales(x, xs, L.K);
+        const int32_t act_group = FP16 ? number(a[11]) : codes_and_scales(x, xs, L.K);
         if (x.size(1) != L.K) throw Refused{"x has as many columns as the layers have inputs"};
         const int64_t M = x.size(0), places = L.places(M);
         PyObject *const epilogue[4] = {rest[0], Py_None, rest[1], rest[2]};
@@ -468,7 +468,7 @@ PyObject *py_experts_linear(PyObject *, PyObject *const *a, Py_ssize_t n)
         {
             py::gil_scoped_release no_gil;
             if (!y.defined()) y = at::empty({places, e.columns}, x.options().dtype(at::kHalf));
-            const mixllm_desc d{(int32_t)M, L.K, L.N, 0, MIXLLM_GROUP, act_group, L.w8_group};
+            const mixllm_desc d{(int32_t)M, L.K, L.N, L.n8, MIXLLM_GROUP, act_group, L.w8_group};
             const mixllm_epilogue ep = e.of(dev);
             const int32_t gather = L.gather ? (int32_t)L.slots.size(1) : 0;
             if (FP16) {

@@ -105,7 +105,7 @@ def test_bad_calls_of_the_experts_are_refused():
     assert experts_call(d, ws=None)[1] == EINVAL
     assert experts_call(binding._desc(0, 256, 64, 0), ptr=None, table=None, offsets=None, rows=None) == (0, 0)
     need = mx.lib().mixllm_experts_workspace
-    assert need(C.byref(d)) == 8 * 256 + 256 and need(C.byref(binding._desc(3, 384, 64, 99, 128))) == 1280 + 256
+    assert need(C.byref(d)) == 8 * 256 + 256 and need(C.byref(binding._desc(3, 384, 64, 9, 128))) == 1280 + 256
 
 
 def test_bad_tables_of_experts_are_refused():
@@ -173,12 +173,12 @@ def test_python_calls_refuse_wrong_operands(monkeypatch):
     refused(lambda: mx.route_experts(logits, 2), "device")
     route = mx.Route(torch.zeros((4, 2), dtype=torch.int32), torch.zeros((4, 2)), torch.zeros(4, dtype=torch.int32), torch.zeros(8, dtype=torch.int32),
                      torch.zeros((4, 2), dtype=torch.int32))
-    E = mx.PackedExperts(256, 64, 256, [L] * 3, u8(3 * 64))
+    E = mx.PackedExperts(256, 64, 256, [L] * 3, u8(3 * 64), 8)
     refused(lambda: mx.experts_linear_fp16(x[:3], E, route), "a row per token")
     refused(lambda: mx.experts_linear_fp16(x, E, route, gather=False), "a row per token")
     refused(lambda: mx.experts_linear_fp16(x[:, :128], E, route), "columns")
     refused(lambda: mx.experts_linear_fp16(x, E, route, bias=half(64)), "bias")
-    refused(lambda: mx.experts_linear_fp16(x, mx.PackedExperts(256, 64, 256, [L] * 2, u8(128)), route), "experts")
+    refused(lambda: mx.experts_linear_fp16(x, mx.PackedExperts(256, 64, 256, [L] * 2, u8(128), 8), route), "experts")
     refused(lambda: mx.experts_linear(x.to(torch.int8), half(4, 2, 1), E, route), "xs")
     refused(lambda: mx.experts_linear_fp16(x, E, route), "device")
     refused(lambda: mx.experts_combine(half(8, 64), route, residual=half(4, 63)), "residual")
