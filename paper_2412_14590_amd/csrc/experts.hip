@@ -47,8 +47,10 @@ static __device__ __forceinline__ TileOf find_tile(LinearParams &p, const Expert
             t8 = (count + BM8 - 1) / BM8 * ((a.table[e].ntiles8 + T16 - 1) / T16);
         }
     };
-    int total4 = 0, total8 = 0;
-    for (int e0 = 0; e0 < a.E; e0 += 64) {
+    int first4, first8;   // of the first 64 experts: kept, the others are read a second time below
+    tiles_of(lane, first4, first8);
+    int total4 = first4, total8 = first8;
+    for (int e0 = 64; e0 < a.E; e0 += 64) {
         int t4, t8;
         tiles_of(e0 + lane, t4, t8);
         total4 += t4;
@@ -65,8 +67,8 @@ static __device__ __forceinline__ TileOf find_tile(LinearParams &p, const Expert
     if (t.none) return t;
     int e = 0, before = 0;
     for (int e0 = 0, sum = 0; e0 < a.E; e0 += 64) {
-        int t4, t8;
-        tiles_of(e0 + lane, t4, t8);
+        int t4 = first4, t8 = first8;
+        if (e0 > 0) tiles_of(e0 + lane, t4, t8);
         const int own = t.part8 ? t8 : t4, upto = sum + wave_scan(own);
         const unsigned long long here = __ballot(own > 0 && L >= upto - own && L < upto);
         if (here) {
