@@ -557,3 +557,23 @@ def test_calls_on_another_stream_and_two_at_once():
                 outs.append(mx.experts_mlp(x, mx.route_experts(logits, 2), UP, DOWN))
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
+
+
+# ---- many short rows ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("M,K", [(2048, 128), (2049, 512), (4099, 640), (2051, 1024), (16384, 1408), (16387, 2048), (16386, 1152)])
+def test_many_short_rows_are_quantized_like_few(M, K):
+    """The inner rows of experts for a prompt: every row gets the codes and the scale that it gets among few rows, rows of zeros
+    and of the largest values among them, and nothing is written behind the last."""
+    gen = torch.Generator(device="cuda").manual_seed(M * 7 + K)
+    x = torch.randn(M, K, generator=gen, device="cuda", dtype=torch.float16)
+    x[5], x[M - 1, K - 1], x[7] = 0, 65504, x[7] * 6e-8
+    xq, xs = torch.full((M + 4, K), 99, dtype=torch.int8, device="cuda"), torch.full((M + 4, 1), 7, dtype=torch.float16, device="cuda")
+    mx.quantize_activations(x, out=(xq[:M], xs[:M]))
+    assert (xq[M:] == 99).all() and (xs[M:] == 7).all()
+    for a in range(0, M, 1000):
+        q, s = mx.quantize_activations(x[a:a + 1000].contiguous())
+        assert torch.equal(q, xq[a:min(a + 1000, M)]) and torch.equal(s.view(torch.int16), xs[a:min(a + 1000, M)].view(torch.int16)), a
+    rows = [0, 5, 7, M - 1]
+    q, s = ref.quantize_act(x[rows].cpu().numpy())
+    assert np.array_equal(q, xq[rows].cpu().numpy()) and np.array_equal(s.reshape(-1), xs[rows].cpu().numpy().reshape(-1))
