@@ -323,7 +323,7 @@ typedef struct mixllm_route_desc {
 } mixllm_route_desc;
 
 /* Bytes of scratch for the call below: 0 up to 16 tokens (one launch), beyond that 2 bytes per expert (rounded up to
- * 8) for each of up to 256 blocks of tokens (two). */
+ * 8) for each of up to 257 blocks of tokens (two). */
 size_t mixllm_route_workspace(const mixllm_route_desc *r);
 /*
  *   logits     fp16 or fp32 [T][logits_stride], aligned to their elements
@@ -385,7 +385,7 @@ int mixllm_experts_linear_fp16(const mixllm_desc *d, int32_t E, const void *tabl
  *   out[t][n] = residual[t][n] + sum_j weights[t][j] * y[slots[t][j]][n]      (fp32, in the order of j; one rounding)
  * A slot of -1 adds nothing.  slots and weights int32 and fp32 [T][top_k] as mixllm_route_experts leaves them (a slot
  * beyond the `places` rows of y adds nothing either); residual fp16 [T][N] or NULL, may be out itself.
- * Errors: EINVAL, EUNSUPPORTED (top_k beyond MIXLLM_MAX_TOP_K), EHIP.
+ * Errors: EINVAL, EUNSUPPORTED (top_k beyond MIXLLM_MAX_TOP_K, T beyond 2^24, N beyond 65535 * 256), EHIP.
  */
 int mixllm_experts_combine(int32_t T, int32_t top_k, int32_t N, int32_t places, const void *y, const float *weights,
                            const int32_t *slots, const void *residual, void *out, void *stream);

@@ -396,6 +396,7 @@ class PackedExperts:
     layers: list            # of PackedLayer: what the table points to
     table: torch.Tensor
     n8: int                 # the most 8-bit channels of any of them
+    pairs: bool = True      # all have an even number of them: gated products can be asked for
 
     @property
     def E(self) -> int:
@@ -408,12 +409,14 @@ def pack_experts(layers) -> PackedExperts:
     assert layers and all((L.K, L.N, L.w8_group, L.perm.device) == (layers[0].K, layers[0].N, layers[0].w8_group, layers[0].perm.device)
                           for L in layers), "experts of one size, granularity and device"
     first = layers[0]
+    assert not first.perm.is_cuda or first.perm.device.index == torch.cuda.current_device(), "layers of the current device"
     entries = (_Expert * len(layers))(*(_Expert(_ptr(L.w4), _ptr(L.w8), _ptr(L.s4), _ptr(L.s8), _ptr(L.z4), _ptr(L.perm), L.n8, 0)
                                         for L in layers))
     table = torch.empty(int(lib().mixllm_experts_table_bytes(len(layers))), dtype=torch.uint8, device=first.perm.device)
     d = first.desc()
     _check(lib().mixllm_experts_table(C.byref(d), len(layers), entries, _ptr(table), _stream()), "mixllm_experts_table")
-    return PackedExperts(first.K, first.N, first.w8_group, layers, table, max(L.n8 for L in layers))
+    return PackedExperts(first.K, first.N, first.w8_group, layers, table, max(L.n8 for L in layers),
+                         all(L.n8 % 2 == 0 for L in layers))
 
 
 def experts_linear(xq: torch.Tensor, xs: torch.Tensor, L: PackedExperts, route: Route, bias=None, activation=None, gated: bool = False,
@@ -421,6 +424,7 @@ def experts_linear(xq: torch.Tensor, xs: torch.Tensor, L: PackedExperts, route: 
     """The linears of the experts over the rows routed to them: y [T * top_k, N] (gated [.., N/2]), one row per assignment in the
     route's order; rows behind the last assignment are left as they were.  gather: xq has a row per token; otherwise one per
     assignment, in the route's order.  bias fp16 [E,N]; activation and gated as in mixed_linear_epilogue."""
+    assert L.pairs or not gated, "gated: every expert has an even number of 8-bit channels"
     return _result(_calls().experts_linear(xq, xs, L.K, L.N, L.w8_group, L.E, L.table, L.n8, route.offsets, route.rows, route.slots, gather, bias,
                                            _named(ACTIVATIONS, activation, "activation"), gated, out, _stream()), "mixllm_experts_linear")
 
@@ -428,6 +432,7 @@ def experts_linear(xq: torch.Tensor, xs: torch.Tensor, L: PackedExperts, route: 
 def experts_linear_fp16(x: torch.Tensor, L: PackedExperts, route: Route, bias=None, activation=None, gated: bool = False,
                         gather: bool = True, act_group=None, out=None, workspace=None) -> torch.Tensor:
     """experts_linear from fp16 activations x [T,K] (gather) or [T * top_k, K]: quantizer and products."""
+    assert L.pairs or not gated, "gated: every expert has an even number of 8-bit channels"
     return _result(_calls().experts_linear_fp16(x, L.K, L.N, L.w8_group, L.E, L.table, L.n8, route.offsets, route.rows, route.slots, gather,
                                                 L.K if act_group is None else act_group, bias,
                                                 _named(ACTIVATIONS, activation, "activation"), gated, out, workspace, _stream()),

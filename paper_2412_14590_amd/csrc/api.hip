@@ -707,7 +707,7 @@ int mixllm_experts_combine(int32_t T, int32_t top_k, int32_t N, int32_t places, 
                            const int32_t *slots, const void *residual, void *out, void *stream)
 {
     if (T < 0 || top_k <= 0 || N <= 0 || places < 0) return MIXLLM_EINVAL;
-    if (top_k > MIXLLM_MAX_TOP_K || T > (1 << 24) || N > (1 << 24)) return MIXLLM_EUNSUPPORTED;
+    if (top_k > MIXLLM_MAX_TOP_K || T > (1 << 24) || N > 65535 * 256) return MIXLLM_EUNSUPPORTED;
     if (T == 0) return MIXLLM_OK;
     if ((places > 0 && (!y || !aligned16(y))) || !weights || ((uintptr_t)weights & 3u) || !slots || ((uintptr_t)slots & 3u) || !out ||
         !aligned16(out) || !aligned16(residual))

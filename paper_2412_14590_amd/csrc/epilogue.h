@@ -23,7 +23,7 @@ static __device__ inline float times_sigmoid(float x, float t) { return x * __bu
 template <int ACT>
 static __device__ inline float activation(float v)
 {
-    if constexpr (ACT == MIXLLM_ACT_RELU) return fmaxf(v, 0.0f);
+    if constexpr (ACT == MIXLLM_ACT_RELU) return v < 0.0f ? 0.0f : v;   // (a NaN stays)
     if constexpr (ACT == MIXLLM_ACT_SILU) return times_sigmoid(v, v);
     // (the complement keeps its relative precision where the sum 1 + erf would cancel)
     if constexpr (ACT == MIXLLM_ACT_GELU) return 0.5f * v * erfcf(-0.70710678118654752f * v);

@@ -47,7 +47,7 @@ static __device__ inline ExpertEntry expert_entry(const ExpertsArgs &a, int e)
 template <bool ROWS>
 static __device__ inline int token_row(const LinearParams &p, int m)
 {
-    if constexpr (ROWS) return p.rows ? min((int)((unsigned)p.rows[m] / (unsigned)p.rows_per_token), p.tokens - 1) : m;
+    if constexpr (ROWS) return p.rows ? (int)min((unsigned)p.rows[m] / (unsigned)p.rows_per_token, (unsigned)(p.tokens - 1)) : m;   // (-1 too)
     return m;
 }
 

@@ -65,7 +65,7 @@ static __device__ __forceinline__ TileOf find_tile(LinearParams &p, const Expert
     const int L = t.part8 ? xcd * per8 + (i - per4) : xcd * per4 + i;
     t.none = t.part8 ? (i - per4 >= per8 || L >= total8) : L >= total4;
     if (t.none) return t;
-    int e = 0, before = 0;
+    int e = -1, before = 0;
     for (int e0 = 0, sum = 0; e0 < a.E; e0 += 64) {
         int t4 = first4, t8 = first8;
         if (e0 > 0) tiles_of(e0 + lane, t4, t8);
@@ -79,6 +79,8 @@ static __device__ __forceinline__ TileOf find_tile(LinearParams &p, const Expert
         }
         sum = uniform(__shfl(upto, 63));
     }
+    t.none = e < 0;   // (lists that say so much that the sums overflow)
+    if (t.none) return t;
     const ExpertEntry x = expert_entry(a, e);
     int first, count;
     expert_rows_uniform(a, e, first, count);
@@ -169,7 +171,7 @@ __global__ __launch_bounds__(256) void experts_combine_kernel(int T, int k, int 
                                                               const int32_t *slots, const half_t *residual, half_t *out)
 {
     typedef half_t vec __attribute__((ext_vector_type(V)));
-    const int n = (blockIdx.x * 256 + threadIdx.x) * V, t = blockIdx.y;
+    const int n = (blockIdx.y * 256 + threadIdx.x) * V, t = blockIdx.x;   // (a grid may have 2^16 blocks in y only)
     if (n >= N) return;
     float sum[V];
 #pragma unroll
@@ -238,7 +240,7 @@ int launch_experts_combine(int T, int k, int N, int places, const void *y, const
 {
     if (T == 0) return (int)hipSuccess;
     auto go = [&](auto kernel, int v) {
-        hipLaunchKernelGGL(kernel, dim3((N + 256 * v - 1) / (256 * v), T), dim3(256), 0, st, T, k, N, places, (const half_t *)y, weights, slots,
+        hipLaunchKernelGGL(kernel, dim3(T, (N + 256 * v - 1) / (256 * v)), dim3(256), 0, st, T, k, N, places, (const half_t *)y, weights, slots,
                            (const half_t *)residual, (half_t *)out);
         return (int)hipGetLastError();
     };

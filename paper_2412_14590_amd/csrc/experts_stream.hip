@@ -84,6 +84,7 @@ struct Shared {
     float sa[MAX_PLACES];              // ... and their scales (one per token)
     uint32_t rowmax[MAX_PLACES];       // scales per token: largest magnitudes of the rows as float bits
     unsigned long long sums[NW];
+    unsigned long long limit;          // tiles of the first MAX_PLACES active experts, where lists name more
     int ranks[NW];
     uint16_t scales[MAX_VALUES / G];   // scales per group: [M][ng] fp16
     __attribute__((aligned(16))) int8_t codes[MAX_VALUES + MAX_PLACES * A_PAD];   // [M][K + A_PAD]
@@ -357,7 +358,8 @@ __global__ __launch_bounds__(NT) void experts_stream_kernel(LinearParams p, Expe
             all += m.sums[w];
             all_ranks += m.ranks[w];
         }
-        if (count > 0 && rank < MAX_PLACES) {   // (as long as the offsets ascend there are no more such experts than places)
+        if (count > 0 && rank == MAX_PLACES) m.limit = x;   // (as long as the offsets ascend there are no more such experts than places)
+        if (count > 0 && rank < MAX_PLACES) {
             uint4 *cell = (uint4 *)&m.active[rank].x;
             cell[0] = words0;
             cell[1] = words1;
@@ -373,12 +375,16 @@ __global__ __launch_bounds__(NT) void experts_stream_kernel(LinearParams p, Expe
         nactive += all_ranks;
         if (e0 + NT < a.E) __syncthreads();
     }
-    nactive = min(uniform(nactive), MAX_PLACES);
+    nactive = uniform(nactive);
     if (tid < a.places) {
         m.tok[tid] = tok;
         m.rowmax[tid] = 0;   // (as many rows as places at most)
     }
     __syncthreads();
+    if (nactive > MAX_PLACES) {
+        nactive = MAX_PLACES;
+        before = m.limit;
+    }
     const unsigned most = (unsigned)a.places * ((unsigned)(p.N + 30) / 16 + 1);
     const int U4 = uniform((int)min((uint32_t)before, most)), U8 = uniform((int)min((uint32_t)(before >> 32), most)), B = gridDim.x;
     auto stage = [&]() {
@@ -423,8 +429,9 @@ __global__ __launch_bounds__(NT) void experts_stream_kernel(LinearParams p, Expe
 
 bool experts_stream_covers(const LinearParams &p, const ExpertsArgs &a)
 {
-    // tiles of a part, in quarters, in 32 bits: every place may be a row tile of its own
-    const long tiles = (long)a.places * ((p.N + 30) / 16 + 1);
+    // tiles of a part, in quarters, in 32 bits: every place may be a row tile of its own, and every expert may have all places in
+    // lists that overlap
+    const long tiles = std::max((long)a.places, (long)a.E * ((a.places + 15) / 16)) * ((p.N + 30) / 16 + 1);
     return a.places <= MAX_PLACES && p.M <= MAX_PLACES && (size_t)p.M * p.K <= (size_t)MAX_VALUES && 4 * tiles < (1l << 31);
 }
 

@@ -401,12 +401,13 @@ __global__ __launch_bounds__(THREADS) void route_lists_kernel(RouteParams p, int
         if (i >= all) p.rows[i] = -1;
 }
 
-// tokens of a block of the counting launch: a power of two from 4 on up to 64, then whole groups of 64 (counts fit 16 bits)
+// Tokens of a block of the counting launch: a power of two from 4 on up to 64, then whole groups of 64; fewer than 2^16, so
+// that a count fits 16 bits where all of them take one expert (2^24 tokens: a block more than MAX_BLOCKS)
 int route_span(int T)
 {
     int span = 4;
     while (span < 64 && (T + span - 1) / span > MAX_BLOCKS) span *= 2;
-    return span < 64 ? span : 64 * ((T + 64 * MAX_BLOCKS - 1) / (64 * MAX_BLOCKS));
+    return span < 64 ? span : 64 * std::min((T + 64 * MAX_BLOCKS - 1) / (64 * MAX_BLOCKS), 1023);
 }
 
 template <int LANES, int SLOTS>

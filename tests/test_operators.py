@@ -188,6 +188,17 @@ def test_epilogue_passes_infinities_and_nan_of_bias_and_residual(M):
     assert torch.equal(y[:, rest], plain[:, rest])
 
 
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("gated", [False, True])
+def test_a_nan_of_the_bias_stays_one(act, gated):
+    for M in (1, 20, 130):
+        PL = pack_from_oracle(layer(256, 40, 4, M, pairs=True))
+        bias = torch.zeros(40, dtype=torch.float16, device="cuda")
+        bias[7] = math.nan
+        y = mx.linear_fp16_epilogue(dev(synth.make_x(M, 256, M)), PL, bias=bias, activation=act, gated=gated)
+        assert bool(torch.isnan(y[:, 3 if gated else 7]).all()) and int(torch.isnan(y).sum()) == M
+
+
 def test_epilogue_of_no_tokens():
     L = layer(256, 32, 4, 1)
     PL = pack_from_oracle(L)
@@ -345,6 +356,16 @@ def test_route_of_no_tokens():
     assert r.ids.shape == (0, 3) and r.rows.numel() == 0 and r.offsets.cpu().tolist() == [0] * 13
 
 
+@pytest.mark.parametrize("T", [(1 << 24) - 16384, 1 << 24])
+def test_route_of_the_most_tokens_to_one_expert(T):
+    logits = torch.zeros((T, 2), dtype=torch.float16, device="cuda")
+    logits[:, 1] = 1
+    r = mx.route_experts(logits, 1)
+    assert r.offsets.cpu().tolist() == [0, 0, T] and bool((r.ids == 1).all()) and bool((r.weights == 1).all())
+    order = torch.arange(T, dtype=torch.int32, device="cuda")
+    assert torch.equal(r.rows, order) and torch.equal(r.slots[:, 0], order)
+
+
 # ---- the experts' products and the sum -------------------------------------------------------------------
 
 def experts(E, K, N, seed, grouped8, shares=None, pairs=False):
@@ -443,6 +464,34 @@ def test_experts_linear_clamps_lists_that_say_too_much():
     assert torch.equal(mx.experts_linear_fp16(x, PE, route), want)
     route.rows[3] = 123456                       # a token that is not there: some token's row instead
     assert torch.equal(mx.experts_linear_fp16(x, PE, route)[:3], want[:3])
+
+
+@pytest.mark.parametrize("M", [4, 40, 200])
+def test_experts_linear_of_lists_without_order(M):
+    """Lists that no route makes give unspecified rows, and nothing else: more experts with rows than places, overlapping ones,
+    some without a part, assignments of no token, with one expert a token and with more."""
+    E = 150
+    layers, PE = experts(E, 256, 34, 3, False)
+    x = dev(synth.make_x(M, 256, 2))
+    rng = np.random.default_rng(M)
+    for k in (1, 2):
+        area = torch.full((M * k + 64, 34), 7.0, dtype=torch.float16, device="cuda")
+        ramp = np.arange(E + 1)
+        for offsets in (ramp % (M * k + 1), ramp % 2 * M * k, rng.integers(-50, M * k + 50, E + 1), ramp[::-1], ramp * 0):
+            rows = rng.integers(-2, M * k + 3, M * k)
+            rows[::3] = -1
+            route = mx.Route(None, None, *(dev(np.ascontiguousarray(a, np.int32)) for a in (offsets, rows, np.zeros((M, k)))))
+            mx.experts_linear_fp16(x, PE, route, out=area[32:32 + M * k])
+            mx.experts_linear(*mx.quantize_activations(x), PE, route, out=area[32:32 + M * k])
+            assert bool((area[:32] == 7).all()) and bool((area[32 + M * k:] == 7).all())
+
+
+def test_combine_of_many_tokens():
+    T = 70000
+    y = torch.arange(T, device="cuda").remainder(2000).half()[:, None].expand(T, 8).contiguous()
+    slots = torch.arange(T - 1, -1, -1, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    route = mx.Route(None, torch.full((T, 1), 0.5, device="cuda"), None, None, slots)
+    assert torch.equal(mx.experts_combine(y, route), y.flip(0) * 0.5)
 
 
 @pytest.mark.parametrize("T,k,N", [(1, 1, 1), (1, 8, 4096), (7, 3, 33), (130, 4, 1000), (61, 32, 24), (300, 2, 8)])

@@ -80,7 +80,10 @@ def test_route_workspace():
     assert need(0, 16) == need(16, 16) == 0
     assert need(17, 16) == 5 * 16 * 2 and need(1025, 16) == 129 * 16 * 2 and need(16384, 16) == 256 * 16 * 2
     assert need(16385, 10) == 129 * 16 * 2               # 128 tokens a block from there on
-    assert need(1 << 24, 1023) == 256 * 1024 * 2
+    assert need((1 << 24) - (1 << 14), 1023) == 256 * 1024 * 2 and need(1 << 24, 1023) == 257 * 1024 * 2
+    # a block's tokens, all with one expert, fit its 16-bit count
+    for T in (17, 100, 16384, 16385, 1 << 20, (1 << 24) - 16384, 1 << 24):
+        assert T <= need(T, 8) // 16 * 0xffff, T
     assert need(10, 1025) == 0                            # (refused)
 
 
@@ -131,6 +134,8 @@ def test_bad_sums_are_refused():
     assert f(4, 0, 64, 8, FAKE, FAKE, FAKE, None, FAKE, None) == EINVAL
     assert f(4, 2, 0, 8, FAKE, FAKE, FAKE, None, FAKE, None) == EINVAL
     assert f(4, 33, 64, 8, FAKE, FAKE, FAKE, None, FAKE, None) == EUNSUPPORTED
+    assert f(4, 2, 65535 * 256 + 1, 8, FAKE, FAKE, FAKE, None, FAKE, None) == EUNSUPPORTED
+    assert f((1 << 24) + 1, 2, 64, 8, FAKE, FAKE, FAKE, None, FAKE, None) == EUNSUPPORTED
     for bad in range(5):
         args = [FAKE, FAKE, FAKE, FAKE, FAKE]
         args[bad] = FAKE + 2
@@ -184,6 +189,9 @@ def test_python_calls_refuse_wrong_operands(monkeypatch):
     refused(lambda: mx.experts_combine(half(8, 64), route, residual=half(4, 63)), "residual")
     refused(lambda: mx.experts_combine(half(8, 64), route, out=half(3, 64)), "out")
     refused(lambda: mx.experts_combine(half(8, 64), route), "device")
+    odd = mx.PackedExperts(256, 64, 256, [L] * 3, u8(3 * 64), 8, pairs=False)
+    refused(lambda: mx.experts_linear_fp16(x, odd, route, gated=True), "even number")
+    refused(lambda: mx.experts_linear(x.to(torch.int8), half(4, 1), odd, route, gated=True), "even number")
     refused(lambda: mx.pack_experts([]), "experts of one size")
     other = binding.PackedLayer(128, 64, 8, 128, L.w8, L.w4, L.s8, L.s4, L.z4, L.perm)
     refused(lambda: mx.pack_experts([L, other]), "experts of one size")
