@@ -8,6 +8,9 @@
 // kernel's output.  Each lane then finishes half of the pair's rows - the even lane the even ones, for which it
 // needs the other's up values, the odd lane the odd ones, for which it needs the gates - so that one exchange
 // between neighbours (a vector instruction) serves two rows and no lane idles in the exponential.
+//
+// It costs what it stores less: K = 1408, N = 4096, 16384 rows 143.1 us without and 141.5 with an empty epilogue, K = 4096, N = 2816 gated with
+// silu 234 and 241; a pass of its own over those sums would read and write 138 MB, 28 us.
 #pragma once
 
 #include <type_traits>

@@ -2,7 +2,7 @@
 // rows per expert that the experts' products read.
 //
 // A token's experts are spread over LANES lanes, SLOTS consecutive experts a lane: a wave for every token, or, where
-// there are tokens enough to fill the chip, 16 lanes, whose maxima are rotations inside a row of lanes (an instruction
+// there are tokens enough, 16 lanes, whose maxima are rotations inside a row of lanes (an instruction
 // each) that serve four tokens at once.  The k experts are found one after the other: the largest key, then the smallest
 // index that has it, so that ties go to the lowest index.  Keys are the logits themselves where score and choice have the
 // same order (no bias, no sum of two scores), which is exact; otherwise score + bias in 64 bits, because two experts whose
@@ -15,7 +15,8 @@
 // one block does it all in one launch; beyond, the first launch leaves the counts of every block and expert, and the
 // second adds up those of the blocks before its own.
 //
-// Bound by instructions and latency, not by the logits' few bytes.
+// Bound by instructions and latency, not by the logits' few bytes: one token of 64 experts 3.8 us (one launch after the other), 61 tokens
+// of 256 in groups 12.3, 16384 tokens of 128 experts, 4 MB of logits, 16 (10 and 6 of the two launches).
 #include <algorithm>
 #include <type_traits>
 
@@ -27,7 +28,9 @@ namespace {
 
 constexpr int THREADS = 1024;
 constexpr int MAX_BLOCKS = 256;   // blocks that the tokens are cut into for counting (a block of the lists reads the counts of all)
-constexpr int ONE_LAUNCH = 16;    // tokens up to which one block takes a wave for each
+// Tokens up to which one block takes a wave for each (us, one launch and two: 64 experts, 4 of them: 1 token 3.8 and 6.8, 16 tokens 6.2 and 7.5,
+// 32 tokens 8.3 and 7.6; 256 experts, 8 of them: 1 token 5.2 and 8.0, 16 tokens 8.8 and 8.8)
+constexpr int ONE_LAUNCH = 16;
 constexpr size_t LDS_CELLS = 140 * 1024;   // LDS for the keys of the waves' tokens, where groups are chosen
 // threads of a block of route_kernel: sixteen 64-bit keys a lane take more than the 128 registers of a block of 1024
 constexpr int threads_of(int slots, bool wide) { return slots == 16 && wide ? 512 : THREADS; }
@@ -454,10 +457,14 @@ int launch_route(const RouteParams &p0, hipStream_t st)
     p.Ep = round_up(p.E, 8);
     // 64-bit keys wherever the order of the choice is not that of the logits
     const bool wide = p.bias || (p.groups > 1 && p.group_top2);
-    // four tokens a wave where a wave for every token would be more than the chip runs at once
-    if (p.T > 16 * cu_count() && p.E <= 256 && p.k <= 16) {
-        if (p.E <= 64) return launch_lanes<16, 4>(p, wide, st);
-        if (p.E <= 128) return launch_lanes<16, 8>(p, wide, st);
+    // Four tokens a wave have fewer instructions a token, a wave for every token the shorter chain, and the more so the more
+    // experts a lane of 16 holds.  us, a wave each and four a wave, 64 experts: 2048 tokens 10.8 and 10.4, 4096 12.2 and 10.4, 16384 20.1
+    // and 12.8; 128 experts: 2048 11.0 and 11.2, 4096 12.8 and 11.6, 16384 24.8 and 17.0; 256 experts: 4096 14.5 and 14.5, 8192 19.5 and 18.1
+    // (with a bias 28.8 and 24.6), 16384 28.9 and 23.7.
+    const int slots = p.E <= 64 ? 4 : p.E <= 128 ? 8 : 16;
+    if (p.T >= 2 * slots * cu_count() && p.E <= 256 && p.k <= 16) {
+        if (slots == 4) return launch_lanes<16, 4>(p, wide, st);
+        if (slots == 8) return launch_lanes<16, 8>(p, wide, st);
         return launch_lanes<16, 16>(p, wide, st);
     }
     if (p.E <= 64) return launch_lanes<64, 1>(p, wide, st);

@@ -285,6 +285,10 @@ ROUTES = [
     dict(T=50, E=257, k=32, bias=True), dict(T=90, E=1024, k=17, groups=2, top_groups=1, bias=True, masked=True), dict(T=33, E=1000, k=10),
     dict(T=70, E=40, k=20), dict(T=2500, E=16, k=2, masked=True), dict(T=5, E=48, k=6, groups=48, top_groups=3, group_score="top2"),
     dict(T=16500, E=4, k=1, half=True),   # more than 256 blocks of 64 tokens
+    # tokens enough for four a wave
+    dict(T=2047, E=64, k=6), dict(T=2049, E=64, k=6, half=True, renormalize=False), dict(T=4099, E=100, k=8, bias=True, masked=True),
+    dict(T=4097, E=128, k=16, groups=8, top_groups=3, group_score="max", half=True), dict(T=4111, E=66, k=5, score="sigmoid", masked=True),
+    dict(T=8193, E=256, k=8, groups=8, top_groups=4, group_score="top2", score="sigmoid", bias=True, scale=2.5), dict(T=8200, E=130, k=1),
 ]
 
 
