@@ -250,8 +250,10 @@ int mixllm_mixed_linear_fp16_static(const mixllm_desc *d, const void *x, const v
  *   y[m][n] = act(v[m][n]) + residual[m][n]                              (gated = 0)
  *   y[m][i] = act(v[m][2 i]) * v[m][2 i + 1] + residual[m][i]            (gated = 1, y is [M][N / 2])
  * Gated, the rows of W alternate: row 2 i is the gate and row 2 i + 1 the up value of output i, N and n8
- * are even, and the list of 8-bit channels holds both rows of a pair or neither (the salience of a pair is
- * that of its rows together).  A list that splits pairs leaves y unspecified (never an access out of bounds).
+ * are even, and the layer's order keeps pairs: feature_perm[2 j] = 2 i and feature_perm[2 j + 1] = 2 i + 1 for every
+ * j < N / 2, each j with an i of its own.  So the list of 8-bit channels holds both rows of a pair or neither (the salience
+ * of a pair is that of its rows together), the gate right before the up value; ascending lists of such pairs do.  The order
+ * lies on the device and is not looked at: any other leaves y unspecified (never an access out of bounds).
  * The residual is added after the activation; `residual` may be y itself (added to in place).  Any of the
  * parts may be absent; with all of them absent y is mixllm_mixed_linear's, up to fp32 rounding.
  * Infinite or NaN values of bias and residual go through the formulas as they are.
@@ -367,7 +369,7 @@ int mixllm_experts_table(const mixllm_desc *d, int32_t E, const mixllm_expert *e
  *   epilogue      bias is [E][N] (or NULL), residual is NULL (it belongs to the sum, mixllm_experts_combine)
  *   y             fp16 [places][N], gated [places][N / 2]; rows from offsets[E] on are left as they were
  * Every row has the sums of mixllm_mixed_linear_epilogue on that row and expert, up to the order of the fp32 additions.
- * Gated, N and every expert's n8 are even.
+ * Gated, N and every expert's n8 are even and every expert's order keeps pairs (as above).
  * Errors: EINVAL, EUNSUPPORTED (M K or a layer's bytes from 2^31 on; E beyond MIXLLM_MAX_EXPERTS), EHIP.
  */
 int mixllm_experts_linear(const mixllm_desc *d, int32_t E, const void *table, const int8_t *xq, const void *xscale,

@@ -185,6 +185,16 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+def _version(t: torch.Tensor):
+    return None if t.is_inference() else t._version
+
+
+def _keeps_pairs(perm):
+    """Of an order with an even number of channels in either part (tensor or numpy array): every even place has an even channel,
+    and the place after it the next."""
+    return ((perm[0::2] % 2 == 0) & (perm[1::2] == perm[0::2] + 1)).all()
+
+
 @dataclass
 class PackedLayer:
     """Packed, quantized weights of one linear layer, resident in HBM."""
@@ -198,6 +208,22 @@ class PackedLayer:
     s4: torch.Tensor
     z4: torch.Tensor
     perm: torch.Tensor      # int32 [N]
+
+    _seen = None   # (perm, its version, n8, whether they keep pairs): what `pairs` found the last time it looked (no field)
+
+    @property
+    def pairs(self) -> bool:
+        """Whether gated products can be asked for: row 2 j of either part is channel 2 i, and row 2 j + 1 channel 2 i + 1.  The order
+        lies on the device: the first look at it waits for it, a later one is free while neither perm nor n8 changes (a list
+        that quantize_weights got from the host was looked at there).  During a capture nothing can be waited for."""
+        seen, version = self._seen, _version(self.perm)
+        if seen is None or seen[0] is not self.perm or seen[1:3] != (version, self.n8):
+            if self.N % 2 or self.n8 % 2:
+                return False
+            assert not (self.perm.is_cuda and torch.cuda.is_current_stream_capturing()), \
+                "gated: whether a layer keeps pairs is not known before its first gated call (or a look at .pairs), which cannot be in a capture"
+            seen = self._seen = (self.perm, version, self.n8, bool(_keeps_pairs(self.perm)))
+        return seen[3]
 
     def desc(self, M=0, act_group=None):
         return _desc(M, self.K, self.N, self.n8, act_group, self.w8_group)
@@ -225,16 +251,19 @@ def quantize_weights(W: torch.Tensor, salient_idx, w8_group=None) -> PackedLayer
     host sequence / numpy array, which is checked (range, duplicates) and copied to the device here."""
     assert W.dtype == torch.float16 and W.dim() == 2
     N, K = W.shape
+    order = None
     if isinstance(salient_idx, torch.Tensor):
         sal = salient_idx.to(device=W.device, dtype=torch.int32).contiguous()
     else:
         host = np.ascontiguousarray(salient_idx, dtype=np.int32)
-        build_feature_perm(N, host)          # raises on an index out of range or a duplicate
+        order = build_feature_perm(N, host)  # raises on an index out of range or a duplicate
         sal = torch.from_numpy(host).to(W.device)
     L = _alloc_layer(K, N, int(sal.numel()), w8_group, W.device)
     d = L.desc()
     _check(lib().mixllm_quantize_weights(C.byref(d), _ptr(W), _ptr(sal), _ptr(L.w8), _ptr(L.w4), _ptr(L.s8),
                                          _ptr(L.s4), _ptr(L.z4), _ptr(L.perm), _stream()), "mixllm_quantize_weights")
+    if order is not None and N % 2 == 0 and L.n8 % 2 == 0:
+        L._seen = (L.perm, _version(L.perm), L.n8, bool(_keeps_pairs(order)))
     return L
 
 
@@ -348,11 +377,19 @@ def _named(table: dict, name, what: str) -> int:
     return table[name]
 
 
+def _check_pairs(L: PackedLayer):
+    # (a layer that is not on the device is refused with the other operands)
+    assert not L.perm.is_cuda or L.pairs, "gated: the layer's order keeps channels 2 i and 2 i + 1 next to each other, in one part (PackedLayer.pairs)"
+
+
 def mixed_linear_epilogue(xq: torch.Tensor, xs: torch.Tensor, L: PackedLayer, bias=None, activation=None, gated: bool = False,
                           residual=None, out=None, workspace=None) -> torch.Tensor:
     """mixed_linear with bias [N], activation (ACTIVATIONS) and residual (of y's shape; may be `out` itself) done on its fp32 sums:
-    y = act(x W^T + bias) + residual.  gated: rows 2 i and 2 i + 1 of W are gate and up of output i, both 8-bit or neither, and
+    y = act(x W^T + bias) + residual.  gated: rows 2 i and 2 i + 1 of W are gate and up of output i and next to each other in the
+    packed layer (L.pairs: both 8-bit or neither; lists of either part in ascending order do), and
     y [M, N/2] = act(gate) up + residual."""
+    if gated:
+        _check_pairs(L)
     return _result(_calls().mixed_linear_epilogue(xq, xs, L.K, L.N, L.n8, L.w8_group, L.w8, L.w4, L.s8, L.s4, L.z4, L.perm, bias, residual,
                                                   _named(ACTIVATIONS, activation, "activation"), gated, out, workspace, _stream()),
                    "mixllm_mixed_linear_epilogue")
@@ -361,6 +398,8 @@ def mixed_linear_epilogue(xq: torch.Tensor, xs: torch.Tensor, L: PackedLayer, bi
 def linear_fp16_epilogue(x: torch.Tensor, L: PackedLayer, bias=None, activation=None, gated: bool = False, residual=None,
                          act_group=None, out=None, workspace=None) -> torch.Tensor:
     """linear_fp16 with the epilogue of mixed_linear_epilogue: fp16 x [M,K] in, fp16 y out, one kernel for a token."""
+    if gated:
+        _check_pairs(L)
     return _result(_calls().linear_fp16_epilogue(x, L.K, L.N, L.n8, L.w8_group, L.w8, L.w4, L.s8, L.s4, L.z4, L.perm,
                                                  L.K if act_group is None else act_group, bias, residual,
                                                  _named(ACTIVATIONS, activation, "activation"), gated, out, workspace, _stream()),
@@ -396,11 +435,24 @@ class PackedExperts:
     layers: list            # of PackedLayer: what the table points to
     table: torch.Tensor
     n8: int                 # the most 8-bit channels of any of them
-    pairs: bool = True      # all have an even number of them: gated products can be asked for
+    pairs: bool = True      # all keep pairs (PackedLayer.pairs): gated products can be asked for
 
     @property
     def E(self) -> int:
         return len(self.layers)
+
+
+def _all_keep_pairs(layers) -> bool:
+    """PackedLayer.pairs of all of them, with one wait for the device."""
+    if any(L.N % 2 or L.n8 % 2 for L in layers):
+        return False
+    new = [L for L in layers if L._seen is None]
+    if new and new[0].perm.is_cuda and torch.cuda.is_current_stream_capturing():
+        return False
+    if new:
+        for L, keeps in zip(new, torch.stack([_keeps_pairs(L.perm) for L in new]).tolist()):
+            L._seen = (L.perm, _version(L.perm), L.n8, keeps)
+    return all(L.pairs for L in layers)
 
 
 def pack_experts(layers) -> PackedExperts:
@@ -415,8 +467,10 @@ def pack_experts(layers) -> PackedExperts:
     table = torch.empty(int(lib().mixllm_experts_table_bytes(len(layers))), dtype=torch.uint8, device=first.perm.device)
     d = first.desc()
     _check(lib().mixllm_experts_table(C.byref(d), len(layers), entries, _ptr(table), _stream()), "mixllm_experts_table")
-    return PackedExperts(first.K, first.N, first.w8_group, layers, table, max(L.n8 for L in layers),
-                         all(L.n8 % 2 == 0 for L in layers))
+    return PackedExperts(first.K, first.N, first.w8_group, layers, table, max(L.n8 for L in layers), _all_keep_pairs(layers))
+
+
+_PAIRS = "gated: every expert has an even number of 8-bit channels, and channels 2 i and 2 i + 1 next to each other in its order (PackedLayer.pairs)"
 
 
 def experts_linear(xq: torch.Tensor, xs: torch.Tensor, L: PackedExperts, route: Route, bias=None, activation=None, gated: bool = False,
@@ -424,7 +478,7 @@ def experts_linear(xq: torch.Tensor, xs: torch.Tensor, L: PackedExperts, route: 
     """The linears of the experts over the rows routed to them: y [T * top_k, N] (gated [.., N/2]), one row per assignment in the
     route's order; rows behind the last assignment are left as they were.  gather: xq has a row per token; otherwise one per
     assignment, in the route's order.  bias fp16 [E,N]; activation and gated as in mixed_linear_epilogue."""
-    assert L.pairs or not gated, "gated: every expert has an even number of 8-bit channels"
+    assert L.pairs or not gated, _PAIRS
     return _result(_calls().experts_linear(xq, xs, L.K, L.N, L.w8_group, L.E, L.table, L.n8, route.offsets, route.rows, route.slots, gather, bias,
                                            _named(ACTIVATIONS, activation, "activation"), gated, out, _stream()), "mixllm_experts_linear")
 
@@ -432,7 +486,7 @@ def experts_linear(xq: torch.Tensor, xs: torch.Tensor, L: PackedExperts, route: 
 def experts_linear_fp16(x: torch.Tensor, L: PackedExperts, route: Route, bias=None, activation=None, gated: bool = False,
                         gather: bool = True, act_group=None, out=None, workspace=None) -> torch.Tensor:
     """experts_linear from fp16 activations x [T,K] (gather) or [T * top_k, K]: quantizer and products."""
-    assert L.pairs or not gated, "gated: every expert has an even number of 8-bit channels"
+    assert L.pairs or not gated, _PAIRS
     return _result(_calls().experts_linear_fp16(x, L.K, L.N, L.w8_group, L.E, L.table, L.n8, route.offsets, route.rows, route.slots, gather,
                                                 L.K if act_group is None else act_group, bias,
                                                 _named(ACTIVATIONS, activation, "activation"), gated, out, workspace, _stream()),
@@ -470,7 +524,8 @@ def channel_salience(W: torch.Tensor, G: torch.Tensor, out=None, weight: float =
 def select_salient(saliences, T: int):
     """The T most salient channels over all layers: `saliences` is a list of fp32 device tensors (one
     per layer); returns one ascending int32 index tensor per layer (on the device) - the salient_idx
-    of quantize_weights for that layer."""
+    of quantize_weights for that layer.  It takes channels one by one.  Of layers for gated products search the pairs:
+    s.view(-1, 2).sum(1) of each, T / 2 of them, and channels 2 p and 2 p + 1 of a pair p."""
     sizes = [int(s.numel()) for s in saliences]
     flat = torch.cat([s.reshape(-1).to(torch.float32) for s in saliences]) if len(saliences) > 1 else \
         saliences[0].reshape(-1).to(torch.float32).contiguous()
