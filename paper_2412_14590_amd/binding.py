@@ -6,7 +6,7 @@ quantized linear runs in the library's own kernels.  There is no fallback: if th
 library is missing the import of `lib()` raises."""
 import ctypes as C
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
 from typing import Optional
 
 import numpy as np
@@ -123,7 +123,8 @@ def lib():
                                                      L.mixllm_mixed_linear_path, L.mixllm_mixed_linear_fp16,
                                                      L.mixllm_mixed_linear_epilogue, L.mixllm_mixed_linear_fp16_epilogue,
                                                      L.mixllm_route_workspace, L.mixllm_route_experts, L.mixllm_experts_workspace,
-                                                     L.mixllm_experts_linear, L.mixllm_experts_linear_fp16, L.mixllm_experts_combine)))
+                                                     L.mixllm_experts_linear, L.mixllm_experts_linear_fp16, L.mixllm_experts_combine,
+                                                     L.mixllm_experts_table_bytes)))
         _native = _calls
         _lib = L
     return _lib
@@ -428,14 +429,17 @@ def route_experts(logits: torch.Tensor, top_k: int, score: str = "softmax", bias
 
 @dataclass
 class PackedExperts:
-    """The packed layers of one linear of a layer of experts, and the device table through which the kernels reach them."""
+    """The packed layers of one linear of a layer of experts, and the device table through which the kernels reach them.  The table
+    holds addresses: the tensors behind them live as long as this does.  Weights written into these tensors are used from then
+    on; a PackedLayer that gets other tensors is another layer, and packed into experts anew."""
     K: int
     N: int
     w8_group: int
-    layers: list            # of PackedLayer: what the table points to
+    layers: tuple           # of PackedLayer: what the table points to
     table: torch.Tensor
     n8: int                 # the most 8-bit channels of any of them
     pairs: bool = True      # all keep pairs (PackedLayer.pairs): gated products can be asked for
+    held: tuple = ()        # the tensors whose addresses the table has
 
     @property
     def E(self) -> int:
@@ -467,7 +471,9 @@ def pack_experts(layers) -> PackedExperts:
     table = torch.empty(int(lib().mixllm_experts_table_bytes(len(layers))), dtype=torch.uint8, device=first.perm.device)
     d = first.desc()
     _check(lib().mixllm_experts_table(C.byref(d), len(layers), entries, _ptr(table), _stream()), "mixllm_experts_table")
-    return PackedExperts(first.K, first.N, first.w8_group, layers, table, max(L.n8 for L in layers), _all_keep_pairs(layers))
+    pairs = _all_keep_pairs(layers)
+    return PackedExperts(first.K, first.N, first.w8_group, tuple(replace(L) for L in layers), table, max(L.n8 for L in layers), pairs,
+                         tuple(t for L in layers for t in (L.w4, L.w8, L.s4, L.s8, L.z4, L.perm)))
 
 
 _PAIRS = "gated: every expert has an even number of 8-bit channels, and channels 2 i and 2 i + 1 next to each other in its order (PackedLayer.pairs)"

@@ -32,6 +32,7 @@ decltype(&mixllm_experts_workspace) experts_workspace;
 decltype(&mixllm_experts_linear) experts_linear;
 decltype(&mixllm_experts_linear_fp16) experts_linear_fp16;
 decltype(&mixllm_experts_combine) experts_combine;
+decltype(&mixllm_experts_table_bytes) experts_table_bytes;
 
 struct Refused {   // what an assertion of the Python side would say
     const char *what;
@@ -433,6 +434,7 @@ struct Experts {
         : K(number(a[0])), N(number(a[1])), w8_group(number(a[2])), E(number(a[3])), n8(number(a[5])), table(tensor(a[4])), offsets(tensor(a[6])),
           rows(tensor(a[7])), slots(tensor(a[8])), gather(truth(a[9]))
     {
+        if (!table.defined() || table.nbytes() < experts_table_bytes(E)) throw Refused{"table: an entry for every expert"};
         list_of(offsets, (int64_t)E + 1, "the route and the layer agree in their experts");
         if (!slots.defined() || slots.dim() != 2 || slots.scalar_type() != at::kInt) throw Refused{"slots: int32, tokens x top_k"};
         list_of(rows, slots.numel(), "rows: int32, one per assignment");
@@ -514,7 +516,7 @@ PyObject *py_experts_combine(PyObject *, PyObject *const *a, Py_ssize_t n)
 // bind(addresses of the library's functions, in the order below)
 PyObject *py_bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    return run(n, 12, [&]() -> PyObject * {
+    return run(n, 13, [&]() -> PyObject * {
         auto take = [&](auto &f, int i) { f = (std::remove_reference_t<decltype(f)>)PyLong_AsVoidPtr(a[i]); };
         take(query_sizes, 0);
         take(quantize_activations, 1);
@@ -528,6 +530,7 @@ PyObject *py_bind(PyObject *, PyObject *const *a, Py_ssize_t n)
         take(experts_linear, 9);
         take(experts_linear_fp16, 10);
         take(experts_combine, 11);
+        take(experts_table_bytes, 12);
         Py_RETURN_NONE;
     });
 }
