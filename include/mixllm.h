@@ -254,7 +254,8 @@ int mixllm_mixed_linear_fp16_static(const mixllm_desc *d, const void *x, const v
  * j < N / 2, each j with an i of its own.  So the list of 8-bit channels holds both rows of a pair or neither (the salience
  * of a pair is that of its rows together), the gate right before the up value; ascending lists of such pairs do.  The order
  * lies on the device and is not looked at: any other leaves y unspecified (never an access out of bounds).
- * The residual is added after the activation; `residual` may be y itself (added to in place).  Any of the
+ * The residual is added after the activation; `residual` may be y itself (added to in place).  Otherwise y overlaps neither the
+ * residual nor the activations, K = N or not: EINVAL.  Any of the
  * parts may be absent; with all of them absent y is mixllm_mixed_linear's, up to fp32 rounding.
  * Infinite or NaN values of bias and residual go through the formulas as they are.
  */
@@ -367,7 +368,8 @@ int mixllm_experts_table(const mixllm_desc *d, int32_t E, const mixllm_expert *e
  *                 number of places.  They stay on the device, so their contents are not validated; places and tokens
  *                 beyond the call's are clamped to it (results unspecified, never an access out of bounds).
  *   epilogue      bias is [E][N] (or NULL), residual is NULL (it belongs to the sum, mixllm_experts_combine)
- *   y             fp16 [places][N], gated [places][N / 2]; rows from offsets[E] on are left as they were
+ *   y             fp16 [places][N], gated [places][N / 2]; rows from offsets[E] on are left as they were; does not overlap the
+ *                 activations (EINVAL)
  * Every row has the sums of mixllm_mixed_linear_epilogue on that row and expert, up to the order of the fp32 additions.
  * Gated, N and every expert's n8 are even and every expert's order keeps pairs (as above).
  * Errors: EINVAL, EUNSUPPORTED (M K or a layer's bytes from 2^31 on; E beyond MIXLLM_MAX_EXPERTS), EHIP.
@@ -386,7 +388,8 @@ int mixllm_experts_linear_fp16(const mixllm_desc *d, int32_t E, const void *tabl
  * Weighted sum of the rows of every token's experts:
  *   out[t][n] = residual[t][n] + sum_j weights[t][j] * y[slots[t][j]][n]      (fp32, in the order of j; one rounding)
  * A slot of -1 adds nothing.  slots and weights int32 and fp32 [T][top_k] as mixllm_route_experts leaves them (a slot
- * beyond the `places` rows of y adds nothing either); residual fp16 [T][N] or NULL, may be out itself.
+ * beyond the `places` rows of y adds nothing either); residual fp16 [T][N] or NULL, may be out itself.  Otherwise out overlaps nothing
+ * that is read (EINVAL).  y, residual and out are 16-byte aligned, whatever N.
  * Errors: EINVAL, EUNSUPPORTED (top_k beyond MIXLLM_MAX_TOP_K, T beyond 2^24, N beyond 65535 * 256), EHIP.
  */
 int mixllm_experts_combine(int32_t T, int32_t top_k, int32_t N, int32_t places, const void *y, const float *weights,

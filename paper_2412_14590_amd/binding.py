@@ -385,7 +385,8 @@ def _check_pairs(L: PackedLayer):
 
 def mixed_linear_epilogue(xq: torch.Tensor, xs: torch.Tensor, L: PackedLayer, bias=None, activation=None, gated: bool = False,
                           residual=None, out=None, workspace=None) -> torch.Tensor:
-    """mixed_linear with bias [N], activation (ACTIVATIONS) and residual (of y's shape; may be `out` itself) done on its fp32 sums:
+    """mixed_linear with bias [N], activation (ACTIVATIONS) and residual (of y's shape; may be `out` itself, which otherwise
+    overlaps no operand) done on its fp32 sums:
     y = act(x W^T + bias) + residual.  gated: rows 2 i and 2 i + 1 of W are gate and up of output i and next to each other in the
     packed layer (L.pairs: both 8-bit or neither; lists of either part in ascending order do), and
     y [M, N/2] = act(gate) up + residual."""
@@ -483,7 +484,8 @@ def experts_linear(xq: torch.Tensor, xs: torch.Tensor, L: PackedExperts, route: 
                    gather: bool = True, out=None) -> torch.Tensor:
     """The linears of the experts over the rows routed to them: y [T * top_k, N] (gated [.., N/2]), one row per assignment in the
     route's order; rows behind the last assignment are left as they were.  gather: xq has a row per token; otherwise one per
-    assignment, in the route's order.  bias fp16 [E,N]; activation and gated as in mixed_linear_epilogue."""
+    assignment, in the route's order.  bias fp16 [E,N]; activation and gated as in mixed_linear_epilogue.  out does not overlap the
+    activations."""
     assert L.pairs or not gated, _PAIRS
     return _result(_calls().experts_linear(xq, xs, L.K, L.N, L.w8_group, L.E, L.table, L.n8, route.offsets, route.rows, route.slots, gather, bias,
                                            _named(ACTIVATIONS, activation, "activation"), gated, out, _stream()), "mixllm_experts_linear")
@@ -500,7 +502,8 @@ def experts_linear_fp16(x: torch.Tensor, L: PackedExperts, route: Route, bias=No
 
 
 def experts_combine(y: torch.Tensor, route: Route, residual=None, out=None) -> torch.Tensor:
-    """Sum of every token's rows of y [T * top_k, N] by the route's weights, plus the residual [T,N] (may be `out` itself)."""
+    """Sum of every token's rows of y [T * top_k, N] by the route's weights, plus the residual [T,N] (may be `out` itself,
+    which otherwise overlaps no operand)."""
     return _result(_calls().experts_combine(y, route.weights, route.slots, residual, out, _stream()), "mixllm_experts_combine")
 
 

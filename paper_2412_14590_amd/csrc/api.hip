@@ -213,6 +213,16 @@ int set_epilogue(const mixllm_desc &d, const mixllm_epilogue *e, LinearParams &p
     return MIXLLM_OK;
 }
 
+// Blocks read activations while others already store results, and each its cells of the residual right before it stores them: y may lie on
+// the residual exactly, on nothing else that the call reads.
+bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    return a && b && na && nb && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+bool residual_ok(const void *residual, const void *y, size_t bytes) { return residual == y || !overlap(residual, bytes, y, bytes); }
+// bytes of y; of a residual, too
+size_t output_bytes(const mixllm_desc &d, size_t rows, const EpilogueArgs &e) { return rows * (size_t)(e.gated ? d.N / 2 : d.N) * sizeof(half_t); }
+
 // Which kernel a call takes: the caller's path argument with AUTO resolved, or a negative status
 // when that path does not cover the shape.  Host arithmetic only; nothing is launched, so that a
 // call can refuse before it has enqueued anything.  `q` receives the parameters the launch uses.
@@ -411,6 +421,8 @@ static int linear_common(const mixllm_desc *d, const int8_t *xq, const void *xsc
         (void)set_epilogue(*d, epilogue, p);   // (checked above)
         const int own = auto_path_epilogue(*d, p);
         if (own == MIXLLM_PATH_PREFILL && !prefill_covers(p)) return MIXLLM_EUNSUPPORTED;
+        const size_t out = output_bytes(*d, (size_t)d->M, p.ep);
+        if (overlap(xq, s.xq_bytes, y, out) || overlap(xscale, s.xscale_bytes, y, out) || !residual_ok(p.ep.residual, y, out)) return MIXLLM_EINVAL;
         return run_epilogue(p, own, (hipStream_t)stream);
     }
     return dispatch(*d, p, path, (hipStream_t)stream);
@@ -464,10 +476,13 @@ static int linear_from_fp16(const mixllm_desc *d, const void *x, const void *pac
     LinearParams p = make_params(*d, nullptr, nullptr, packed_w4, packed_w8, scales4, scales8, zeros4, feature_perm);
     p.y = (half_t *)y;
     p.ep = checked.ep;
+    const size_t out = output_bytes(*d, (size_t)d->M, p.ep);
+    const bool clash = epilogue && (overlap(x, 2 * s.xq_bytes, y, out) || !residual_ok(p.ep.residual, y, out));
     // One kernel when a decode variant can quantize inside the linear: every block then repeats the
     // quantizer, so the variants only offer it where that measured cheaper than the stand-alone
     // kernel's launch and round trips (one token; a few tokens of a short row).
     if (decode_can_fuse_quantizer(p)) {
+        if (clash) return MIXLLM_EINVAL;
         p.x = (const half_t *)x;
         const int e = epilogue ? (decode_split_covers(p) ? launch_split_epilogue(p, st) : (int)hipErrorInvalidValue) : launch_linear_decode(p, st);
         if (e != (int)hipErrorInvalidValue) return hip_status(e);
@@ -491,6 +506,7 @@ static int linear_from_fp16(const mixllm_desc *d, const void *x, const void *pac
     int path = epilogue ? auto_path_epilogue(*d, p) : resolve_path(*d, p, MIXLLM_PATH_AUTO, q);
     if (epilogue && path == MIXLLM_PATH_PREFILL && !prefill_covers(p)) path = MIXLLM_EUNSUPPORTED;
     if (path < 0) return path;
+    if (clash) return MIXLLM_EINVAL;
     if (int rc = hip_status(launch_quantize_activations(*d, x, xq, xscale, st))) return rc;
     return epilogue ? run_epilogue(q, path, st) : run_path(q, path, st);
 }
@@ -676,6 +692,10 @@ static int experts_common(const mixllm_desc *d0, int32_t E, const void *table, c
         p.xscale = (const half_t *)((uint8_t *)workspace + xq_bytes);
     } else if (!xq || !aligned16(xq) || !xscale || !aligned16(xscale))
         return MIXLLM_EINVAL;
+    mixllm_sizes s;
+    sizes_of(d, s);
+    const size_t out = output_bytes(d, (size_t)places, p.ep);
+    if (overlap(x, 2 * s.xq_bytes, y, out) || overlap(xq, s.xq_bytes, y, out) || overlap(xscale, s.xscale_bytes, y, out)) return MIXLLM_EINVAL;
     p.y = (half_t *)y;
     p.rows = gather ? rows : nullptr;
     p.rows_per_token = std::max(gather, 1);
@@ -711,6 +731,10 @@ int mixllm_experts_combine(int32_t T, int32_t top_k, int32_t N, int32_t places, 
     if (T == 0) return MIXLLM_OK;
     if ((places > 0 && (!y || !aligned16(y))) || !weights || ((uintptr_t)weights & 3u) || !slots || ((uintptr_t)slots & 3u) || !out ||
         !aligned16(out) || !aligned16(residual))
+        return MIXLLM_EINVAL;
+    const size_t row = (size_t)N * sizeof(half_t), cells = (size_t)T * top_k * 4;
+    if (overlap(y, places * row, out, T * row) || overlap(weights, cells, out, T * row) || overlap(slots, cells, out, T * row) ||
+        !residual_ok(residual, out, T * row))
         return MIXLLM_EINVAL;
     return hip_status(launch_experts_combine(T, top_k, N, places, y, weights, slots, residual, out, (hipStream_t)stream));
 }

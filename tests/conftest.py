@@ -14,7 +14,7 @@ def pytest_configure(config):
 
 # Host-side checks of the C entries pass made-up addresses: calls that a check refuses, but also calls that only the absence of a
 # GPU ends.  With a GPU those would launch kernels on these addresses.
-MADE_UP_ADDRESSES = {"test_host_api.py", "test_operators_host.py"}
+MADE_UP_ADDRESSES = {"test_host_api.py", "test_operators_host.py", "test_operators_overlap_host.py"}
 
 
 def pytest_collection_modifyitems(config, items):
