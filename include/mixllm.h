@@ -372,7 +372,8 @@ int mixllm_experts_table(const mixllm_desc *d, int32_t E, const mixllm_expert *e
  *                 activations (EINVAL)
  * Every row has the sums of mixllm_mixed_linear_epilogue on that row and expert, up to the order of the fp32 additions.
  * Gated, N and every expert's n8 are even and every expert's order keeps pairs (as above).
- * Errors: EINVAL, EUNSUPPORTED (M K or a layer's bytes from 2^31 on; E beyond MIXLLM_MAX_EXPERTS), EHIP.
+ * Errors: EINVAL, EUNSUPPORTED (M K or a layer's bytes from 2^31 on; E beyond MIXLLM_MAX_EXPERTS; more than 2^24 tiles, of 128
+ * channels and 32 to 128 rows, one that is not full for every expert), EHIP.
  */
 int mixllm_experts_linear(const mixllm_desc *d, int32_t E, const void *table, const int8_t *xq, const void *xscale,
                           const int32_t *offsets, const int32_t *rows, int32_t gather,

@@ -701,7 +701,9 @@ static int experts_common(const mixllm_desc *d0, int32_t E, const void *table, c
     p.rows_per_token = std::max(gather, 1);
     p.tokens = d.M;
     ExpertsArgs a{(const ExpertEntry *)table, offsets, E, (int)places, d.n8};
-    if (x && experts_stream_covers(p, a)) p.x = (const half_t *)x;   // one kernel
+    const bool stream = x && experts_stream_covers(p, a);
+    if (!stream && !experts_tiled_covers(p, a)) return MIXLLM_EUNSUPPORTED;
+    if (stream) p.x = (const half_t *)x;   // one kernel
     else if (x)
         if (int rc = hip_status(launch_quantize_activations(d, x, (int8_t *)p.xq, (void *)p.xscale, st))) return rc;
     return hip_status(launch_experts_linear(p, a, st));

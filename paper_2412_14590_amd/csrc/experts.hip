@@ -14,6 +14,8 @@ namespace mixllm {
 
 namespace {
 
+constexpr long MAX_WORK_ITEMS = (1l << 32) - 1;   // blocks times threads of a launch, in x
+
 constexpr int TABLE_CHUNK = 32;   // entries that travel as arguments of one launch
 struct TableChunk {
     ExpertEntry entry[TABLE_CHUNK];
@@ -144,16 +146,21 @@ __global__ __launch_bounds__(C::THREADS, 2) void experts_tiled_kernel(LinearPara
     else pick(C{}, tile4);
 }
 
+// the most tiles, as blocks: every expert with rows may have a row tile that is not full; the 4-bit part is at most the layer, the
+// 8-bit part the largest of any expert (a.n8).  Blocks without a tile live for a microsecond.
 template <typename C>
-int launch_experts_shape(const LinearParams &p, const ExpertsArgs &a, hipStream_t st)
+long blocks_of(const LinearParams &p, const ExpertsArgs &a)
 {
-    // the most tiles: every expert with rows may have a row tile that is not full; the 4-bit part is at most the layer, the
-    // 8-bit part the largest of any expert (a.n8).  Blocks without a tile live for a microsecond.
     const long busy = std::min(a.E, a.places);
     const long tiles4 = (a.places / C::BM + busy) * ((round_up(p.N, TILE_N) + C::BN - 1) / C::BN);
     const long tiles8 = (a.places / C::Half::BM + busy) * ((round_up(a.n8, TILE_N) + C::BN - 1) / C::BN);
-    const long blocks = 8 * ((tiles4 + 7) / 8 + (tiles8 + 7) / 8);
-    if (blocks >= (1l << 31)) return (int)hipErrorInvalidValue;
+    return 8 * ((tiles4 + 7) / 8 + (tiles8 + 7) / 8);
+}
+
+template <typename C>
+int launch_experts_shape(const LinearParams &p, const ExpertsArgs &a, hipStream_t st)
+{
+    const long blocks = blocks_of<C>(p, a);
     auto go = [&](auto kernel, bool grouped) {
         const size_t lds = (size_t)NSTAGE * C::A_STAGE + token_scale_bytes(grouped, C::BM);
         if (int e = ensure_dynamic_lds((const void *)kernel, lds)) return e;
@@ -220,30 +227,48 @@ bool experts_cover(const LinearParams &p)
     return (size_t)p.M * p.K < lim && (size_t)(p.N + 30) * p.K < lim;
 }
 
+// The height of the row tiles, by the rows of an expert on average (which experts they go to is known on the device only).
+// A higher tile reads the weights and unpacks them less often, a lower one starts sooner and shares out better.  64 experts,
+// K 4096, N 2816, the products alone, us with 32, 64, 128 rows: mean 8: 76.5, 78.3, 83.7; 16: 85.8, 85.5, 94.1; 32: 101, 99, 107;
+// 64: 145, 128, 130; 96: 189, 161, 158; 256: 414, 345, 317.  With scales per 128 channels the partial sums leave no registers
+// for 128 rows: mean 16: 89.8, 91.5; 32: 121, 111; 128: 281, 227.
+template <typename F>
+static auto with_shape(const LinearParams &p, const ExpertsArgs &a, F &&f)
+{
+    const long mean = a.places / a.E;
+    if (mean > 64 && p.act_per_token) return f(Shape<1, 4, 4, MIXLLM_PREFILL_WD_LARGE>{});
+    if (mean > 16) return f(Shape<1, 4, 2, MIXLLM_PREFILL_WD_SMALL>{});
+    return f(Shape<1, 4, 1, MIXLLM_PREFILL_WD_SMALL>{});
+}
+
+bool experts_tiled_covers(const LinearParams &p, const ExpertsArgs &a)
+{
+    return with_shape(p, a, [&](auto shape) { return blocks_of<decltype(shape)>(p, a) <= MAX_WORK_ITEMS / decltype(shape)::THREADS; });
+}
+
 int launch_experts_linear(const LinearParams &p, const ExpertsArgs &a, hipStream_t st)
 {
     if (!experts_cover(p)) return (int)hipErrorInvalidValue;
     if (a.places == 0) return (int)hipSuccess;
     if (p.x) return launch_experts_stream(p, a, st);
-    // The height of the row tiles, by the rows of an expert on average (which experts they go to is known on the device only).
-    // A higher tile reads the weights and unpacks them less often, a lower one starts sooner and shares out better.  64 experts,
-    // K 4096, N 2816, the products alone, us with 32, 64, 128 rows: mean 8: 76.5, 78.3, 83.7; 16: 85.8, 85.5, 94.1; 32: 101, 99, 107;
-    // 64: 145, 128, 130; 96: 189, 161, 158; 256: 414, 345, 317.  With scales per 128 channels the partial sums leave no registers
-    // for 128 rows: mean 16: 89.8, 91.5; 32: 121, 111; 128: 281, 227.
-    const long mean = a.places / a.E;
-    if (mean > 64 && p.act_per_token) return launch_experts_shape<Shape<1, 4, 4, MIXLLM_PREFILL_WD_LARGE>>(p, a, st);
-    if (mean > 16) return launch_experts_shape<Shape<1, 4, 2, MIXLLM_PREFILL_WD_SMALL>>(p, a, st);
-    return launch_experts_shape<Shape<1, 4, 1, MIXLLM_PREFILL_WD_SMALL>>(p, a, st);
+    if (!experts_tiled_covers(p, a)) return (int)hipErrorInvalidValue;
+    return with_shape(p, a, [&](auto shape) { return launch_experts_shape<decltype(shape)>(p, a, st); });
 }
 
 int launch_experts_combine(int T, int k, int N, int places, const void *y, const float *weights, const int32_t *slots, const void *residual,
                            void *out, hipStream_t st)
 {
     if (T == 0) return (int)hipSuccess;
+    constexpr int MOST = 1 << 23;   // tokens of a launch: a block of 256 threads each
     auto go = [&](auto kernel, int v) {
-        hipLaunchKernelGGL(kernel, dim3(T, (N + 256 * v - 1) / (256 * v)), dim3(256), 0, st, T, k, N, places, (const half_t *)y, weights, slots,
-                           (const half_t *)residual, (half_t *)out);
-        return (int)hipGetLastError();
+        for (int t = 0; t < T; t += MOST) {
+            const size_t cell = (size_t)t * N, choice = (size_t)t * k;
+            hipLaunchKernelGGL(kernel, dim3(std::min(T - t, MOST), (N + 256 * v - 1) / (256 * v)), dim3(256), 0, st, std::min(T - t, MOST), k, N, places,
+                               (const half_t *)y, weights + choice, slots + choice, residual ? (const half_t *)residual + cell : nullptr,
+                               (half_t *)out + cell);
+            if (hipError_t e = hipGetLastError()) return (int)e;
+        }
+        return (int)hipSuccess;
     };
     return N % 8 == 0 ? go(experts_combine_kernel<8>, 8) : go(experts_combine_kernel<1>, 1);
 }

@@ -300,6 +300,8 @@ struct ExpertsArgs {
 };
 int launch_experts_table(int E, int N, const mixllm_expert *experts, ExpertEntry *table, hipStream_t st);
 bool experts_cover(const LinearParams &p);
+// whether the grid of tiles of all that lists may hold can be launched
+bool experts_tiled_covers(const LinearParams &p, const ExpertsArgs &a);
 // kernel for a token or a few, from fp16 activations (p.x) that it quantizes itself (experts_stream.hip)
 bool experts_stream_covers(const LinearParams &p, const ExpertsArgs &a);
 int launch_experts_stream(const LinearParams &p, const ExpertsArgs &a, hipStream_t st);
