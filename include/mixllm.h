@@ -296,8 +296,9 @@ int mixllm_mixed_linear_fp16_epilogue(const mixllm_desc *d, const void *x, const
  * Choice: c_e = s_e + bias_e, in 64 bits (a NaN or -infinity is not selectable).  With groups > 1 the experts fall
  * into `groups` consecutive groups of E / groups; a group's score is its largest c_e, or the sum of its two largest,
  * and only the experts of the top_groups groups with the largest scores stay selectable.  Of those the top_k largest
- * c_e are taken, the largest first.  Ties go to the lowest index, of groups and of experts; equal are values that are equal
- * as the real numbers above where there is neither a bias nor a sum of two, and their 64-bit values otherwise.
+ * c_e are taken, the largest first.  Ties go to the lowest index, of groups and of experts.  Where there is neither a bias nor
+ * a sum of two the choice goes by the logits, whose order is that of the scores as real numbers: ties are equal logits.  (Beside a
+ * logit of +infinity a softmax gives all finite ones 0; they are still taken the largest first.)  Otherwise by c_e in 64 bits.
  *   ids      [T][top_k]  the experts taken; -1 where fewer than top_k are selectable
  *   weights  [T][top_k]  s_e of the experts taken (without the bias), 0 beside an id of -1; renormalize: divided by their
  *                        sum (0 where that is 0); then times scale
