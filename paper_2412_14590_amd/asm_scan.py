@@ -23,6 +23,7 @@ _BRANCH = re.compile(r"^(s_cbranch_\w+|s_branch)\s+([.\w$]+)")
 _VRANGE = re.compile(r"\bv\[(\d+):(\d+)\]")
 _VONE = re.compile(r"\bv(\d+)\b")
 _VMCNT = re.compile(r"vmcnt\((\d+)\)")
+_DRAINED = "; ring drained"   # left by a source where none of its hand-issued loads is in flight any more
 _CAP = 64   # the counter has six bits: nothing is ever younger than that
 
 
@@ -51,8 +52,11 @@ def _functions(asm_text):
     """(name, [(line number, text, inside inline asm) | label]) for every function of the file."""
     funcs, cur, name, in_asm = [], None, None, False
     types = set(re.findall(r"\.type\s+([.\w$]+),@function", asm_text))
+    if not types:   # a piece of a listing
+        cur = []
+        funcs.append(("", cur))
     for i, raw in enumerate(asm_text.split("\n"), 1):
-        t = raw.split(";")[0].strip() if not raw.strip().startswith(";;#") else raw.strip()
+        t = raw.strip() if raw.strip().startswith((";;#", _DRAINED)) else raw.split(";")[0].strip()
         if t.startswith(";;#ASMSTART"):
             in_asm = True
             continue
@@ -135,46 +139,51 @@ def _step(state, it, report):
         report(it, hit, state)
 
 
+def _entry_states(blocks, start, step, merge):
+    """State before every block (None where no path leads): step(state, instruction) changes a state in place, merge(into, state) takes another
+    path's in and says whether that changed anything.  A branch to a label that is not in the listing counts as falling through."""
+    index = {lab: b for b, (labels, _, _, _) in enumerate(blocks) for lab in labels}
+    entry = [None] * len(blocks)
+    if blocks:
+        entry[0] = dict(start)
+    work = [0] if blocks else []
+    while work:
+        b = work.pop()
+        _, ins, targets, fall = blocks[b]
+        state = dict(entry[b])
+        for it in ins:
+            step(state, it)
+        to = [index[x] for x in targets if x in index]
+        if (fall or len(to) < len(targets)) and b + 1 < len(blocks):
+            to.append(b + 1)
+        for t in to:
+            if entry[t] is None:
+                entry[t] = dict(state)
+                work.append(t)
+            elif merge(entry[t], state):
+                work.append(t)
+    return entry
+
+
+def _merge_least(into, state):
+    """Least number per key; a key that one side lacks counts as far away."""
+    changed = False
+    for r, v in state.items():
+        if r not in into or into[r] > v:
+            into[r] = v
+            changed = True
+    return changed
+
+
 def check_hand_issued_loads(asm_text, name):
     """Raise RuntimeError when a path through a kernel of `asm_text` touches the destination of a
     hand-issued load before a wait has retired it."""
     bad = []
     for fname, items in _functions(asm_text):
         blocks = _blocks(items)
-        index = {}
-        for b, (labels, _, _, _) in enumerate(blocks):
-            for lab in labels:
-                index[lab] = b
-        succs = []
-        for b, (_, _, targets, fall) in enumerate(blocks):
-            s = [index[x] for x in targets if x in index]
-            if fall and b + 1 < len(blocks):
-                s.append(b + 1)
-            succs.append(s)
-        entry = [None] * len(blocks)
-        entry[0] = {}
-        work = [0]
-        while work:
-            b = work.pop()
-            state = dict(entry[b])
-            for it in blocks[b][1]:
-                _step(state, it, None)
-            for s in succs[b]:
-                if entry[s] is None:
-                    entry[s] = dict(state)
-                    work.append(s)
-                    continue
-                changed = False
-                for r, (y, ln) in state.items():
-                    if r not in entry[s] or entry[s][r][0] > y:
-                        entry[s][r] = (y, ln)
-                        changed = True
-                if changed:
-                    work.append(s)
-        for b, (_, ins, _, _) in enumerate(blocks):
-            if entry[b] is None:
+        for (_, ins, _, _), state in zip(blocks, _entry_states(blocks, {}, lambda st, it: _step(st, it, None), _merge_least)):
+            if state is None:
                 continue
-            state = dict(entry[b])
 
             def report(it, hit, st):
                 r = min(hit)
@@ -185,3 +194,99 @@ def check_hand_issued_loads(asm_text, name):
                 _step(state, it, report)
     if bad:
         raise RuntimeError(f"{len(bad)} uses of registers whose hand-issued loads may still be in flight:\n  " + "\n  ".join(bad[:12]))
+
+
+_SREG = re.compile(r"\bs(\d+)\b|\bs\[(\d+):(\d+)\]|\b(vcc)(_lo|_hi)?\b")
+# scalar instructions whose first operand is not (or not always) written
+_SCALAR_NO_WRITE = ("s_cmp", "s_bitcmp", "s_cbranch", "s_branch", "s_waitcnt", "s_nop", "s_barrier", "s_setprio", "s_sleep", "s_endpgm", "s_setreg",
+                    "s_sendmsg", "s_setpc", "s_cmov", "s_trap", "s_sethalt", "s_set_gpr")
+SCALAR_WAIT = 5   # wait states between a vector instruction that writes a scalar register and a vector-memory one that reads it
+
+
+def _sregs(text):
+    out = set()
+    for one, a, b, vcc, half in _SREG.findall(text):
+        if one:
+            out.add(int(one))
+        elif vcc:
+            out |= {106, 107} if not half else {106 if half == "_lo" else 107}
+        else:
+            out |= set(range(int(a), int(b) + 1))
+    return out
+
+
+def _scalar_step(state, it):
+    """Advance `state` (scalar register -> wait states since a vector instruction wrote it, while fewer than SCALAR_WAIT)."""
+    t = it.text
+    if t.startswith(";"):
+        return
+    passed = 1 + (int(t.split()[1], 0) if t.startswith("s_nop") else 0)
+    for r in list(state):
+        state[r] += passed
+        if state[r] >= SCALAR_WAIT:
+            del state[r]
+    ops = t.split(None, 1)[1].split(",") if " " in t or "\t" in t else []
+    if t.startswith("v_"):
+        dst = _sregs(ops[0]) if ops else set()
+        if len(ops) > 1 and ("_co_" in t.split()[0] or t.startswith(("v_div_scale", "v_mad_u64", "v_mad_i64"))):
+            dst |= _sregs(ops[1])   # the carry
+        state.update(dict.fromkeys(dst, 0))
+    elif t.startswith("s_") and not t.startswith(_SCALAR_NO_WRITE) and ops:
+        for r in _sregs(ops[0]):
+            state.pop(r, None)
+
+
+def check_scalar_bases(asm_text, name):
+    """A scalar register written by a vector instruction - a lane read, the reload of a scalar spilled to a vector register's lanes, a
+    comparison - may be read by a vector-memory instruction only SCALAR_WAIT wait states later.  The compiler fills them in in front of
+    its own loads, but not in front of one inside an asm statement, whose base is then a stale address.  Raise RuntimeError when any
+    path of the control-flow graph comes to a hand-issued load too soon."""
+    bad = []
+    for fname, items in _functions(asm_text):
+        blocks = _blocks(items)
+        for (_, ins, _, _), state in zip(blocks, _entry_states(blocks, {}, _scalar_step, _merge_least)):
+            if state is None:
+                continue
+            for it in ins:
+                if it.hand and it.text.startswith("global_load_"):
+                    close = _sregs(it.text) & state.keys()
+                    if close:
+                        bad.append(f"{name}.s:{it.line}: {fname[:60]} `{it.text[:70]}` reads s{sorted(close)}, written by a vector instruction less "
+                                   f"than {SCALAR_WAIT} wait states before")
+                _scalar_step(state, it)
+    if bad:
+        raise RuntimeError("hand-issued loads read scalar registers too early:\n  " + "\n  ".join(bad[:10]))
+
+
+def _is_ring_load(it):
+    """A load of a decode kernel's ring: weights (non-temporal), and their scales and zero points."""
+    return it.hand and (re.match(r"global_load_dwordx4 .* nt$", it.text) is not None or it.text.startswith(("global_load_dwordx2", "global_load_ushort")))
+
+
+def _ring_step(state, it):
+    """Advance `state` (registers that a load of the ring was issued into and that may be part of it still: until the source says that
+    the ring is drained)."""
+    if _is_ring_load(it):
+        state.update(dict.fromkeys(_vregs(it.text.split(",")[0]), 0))
+    elif it.text.startswith(_DRAINED):
+        state.clear()
+
+
+def ring_copies(asm_text, kernel):
+    """(function, copies) for every function with `kernel` in its name: its VGPR-to-VGPR copies that name a register of the ring, on
+    any path on which a load of the ring was issued into it before and the ring was not drained since.  (The activation loads are
+    consumed before the loop and their registers reused.)"""
+    out = []
+    for fname, items in _functions(asm_text):
+        if kernel not in fname:
+            continue
+        blocks, n = _blocks(items), 0
+        for (_, ins, _, _), state in zip(blocks, _entry_states(blocks, {}, _ring_step, _merge_least)):
+            if state is None:
+                continue
+            for it in ins:
+                if re.match(r"v_(mov_b(32|64)_e32|swap_b32) v[\[\d][^,]*, v[\[\d]", it.text) and _vregs(it.text) & state.keys():
+                    n += 1
+                _ring_step(state, it)
+        out.append((fname, n))
+    return out

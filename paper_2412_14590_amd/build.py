@@ -109,34 +109,7 @@ def check_hand_issued_loads(asm_text: str, name: str) -> None:
 
 
 def check_scalar_bases(asm_text: str, name: str) -> None:
-    """A scalar register written by a vector instruction - a lane read, or the reload of a scalar spilled to a vector
-    register's lanes - may be read by a vector-memory instruction only 5 wait states later.  The compiler fills them in
-    in front of its own loads, but not in front of one inside an asm statement, whose base is then a stale address."""
-    def scalars(text):
-        out = set()
-        for a, b in re.findall(r"\bs\[(\d+):(\d+)\]", text):
-            out |= set(range(int(a), int(b) + 1))
-        return out | {int(a) for a in re.findall(r"\bs(\d+)\b", text)}
-    written, now, in_asm, bad = {}, 0, False, []
-    for i, line in enumerate(asm_text.split("\n"), 1):
-        t = line.strip()
-        if t.startswith((";;#ASMSTART", ";;#ASMEND")):
-            in_asm = t.startswith(";;#ASMSTART")
-            continue
-        if not t or t[0] in ";." or t.endswith(":"):
-            continue
-        if in_asm and t.startswith("global_load_"):
-            close = [r for r in scalars(t) if now - written.get(r, -9) < 5]
-            if close:
-                bad.append(f"{name}.s:{i}: `{t[:70]}` reads s{sorted(close)}, written by a vector instruction less than 5 wait states before")
-        now += 1 + (int(t.split()[1], 0) if t.startswith("s_nop") else 0)
-        if t.startswith(("v_readlane", "v_readfirstlane")):
-            written.update(dict.fromkeys(scalars(t.split(",")[0]), now))
-        elif t.startswith("s_"):
-            for r in scalars(t.split(",")[0]):
-                written.pop(r, None)
-    if bad:
-        raise RuntimeError("hand-issued loads read scalar registers too early:\n  " + "\n  ".join(bad[:10]))
+    asm_scan.check_scalar_bases(asm_text, name)
 
 
 # Sources whose kernels pass the path-following scan of asm_scan.py (every path through the control-flow
@@ -148,37 +121,17 @@ FULL_SCAN = {"linear_prefill.hip", "epilogue_tiled.hip", "experts.hip", "experts
 # stay where they are.  Where the loop nest makes the compiler rotate them (seen with the chunk loop of
 # the evenly split decode kernel nested in a loop over activation windows: 80 to 220 copies, at the loop
 # latch, of registers whose loads were still in flight; the late data then landed in registers that
-# held addresses by then) the kernel has dozens of register-to-register copies of them; as built it
-# has none, or a handful that copy a thread index into a register the ring used earlier.
-RING_COPY_LIMIT = {s: ("linear_decode_split_kernel", 8) for s in ("linear_decode_split.hip", "epilogue_decode_split.hip")}
+# held addresses by then) the kernel has dozens of register-to-register copies of them; as built it has none on any path
+# between a request and the end of the ring.
+RING_COPY_LIMIT = {s: ("linear_decode_split_kernel", 0) for s in ("linear_decode_split.hip", "epilogue_decode_split.hip")}
 
 
 def check_ring_copies(asm_text: str, src: str) -> None:
-    """Tripwire: count, per kernel, the VGPR-to-VGPR copies that name a destination register of a
-    hand-issued load of the ring (the activation loads are consumed before the loop and their
-    registers reused); fail above RING_COPY_LIMIT.  Where the source marks the ring as drained nothing is in flight
-    until the next of its loads: an epilogue there copies what it likes."""
+    """Tripwire: count, per kernel, the register-to-register copies of the ring (asm_scan.ring_copies); fail above RING_COPY_LIMIT."""
     kernel, limit = RING_COPY_LIMIT[src]
-    lines = asm_text.split("\n")
-    for st in [i for i, l in enumerate(lines) if re.match(r"^_Z\S*" + kernel + r"\S*:", l)]:
-        end = next((i for i in range(st, len(lines)) if "s_endpgm" in lines[i]), len(lines))
-        hand, copies, in_asm, drained = set(), [], False, False
-        for l in lines[st:end]:
-            t = l.strip()
-            if t.startswith(";;#ASMSTART"):
-                in_asm = True
-            elif t.startswith(";;#ASMEND"):
-                in_asm = False
-            elif in_asm and (re.match(r"global_load_dwordx4 .* nt$", t) or t.startswith(("global_load_dwordx2", "global_load_ushort"))):
-                drained = False
-                hand |= _vregs(t.split(",")[0])   # weights (non-temporal) and their scales and zero points: the ring
-            elif in_asm and t == "; ring drained":
-                drained = True
-            elif not drained and re.match(r"v_(mov_b(32|64)_e32|swap_b32) v[\[\d][^,]*, v[\[\d]", t):
-                copies.append(t)
-        n = sum(1 for c in copies if _vregs(c) & hand)
+    for name, n in asm_scan.ring_copies(asm_text, kernel):
         if n > limit:
-            raise RuntimeError(f"{lines[st].split(':')[0]}: {n} register copies of hand-loaded registers (limit {limit}): "
+            raise RuntimeError(f"{name}: {n} register copies of hand-loaded registers (limit {limit}): "
                                "the compiler is moving a ring of loads that may be in flight")
 
 
