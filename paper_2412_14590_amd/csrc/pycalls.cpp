@@ -101,10 +101,14 @@ bool overrides_new_empty(PyObject *o)
 {
     return !THPVariable_CheckExact(o) || at::impl::torch_function_mode_enabled();
 }
-at::Tensor new_empty_in_python(PyObject *o, int64_t rows, int64_t columns, at::ScalarType type)
+at::Tensor new_empty_in_python(PyObject *o, const py::tuple &sizes, at::ScalarType type)
 {
     const auto dtype = py::reinterpret_borrow<py::object>((PyObject *)torch::getTHPDtype(type));
-    return tensor(py::handle(o).attr("new_empty")(py::make_tuple(rows, columns), py::arg("dtype") = dtype).ptr());
+    return tensor(py::handle(o).attr("new_empty")(sizes, py::arg("dtype") = dtype).ptr());
+}
+at::Tensor new_empty_in_python(PyObject *o, int64_t rows, int64_t columns, at::ScalarType type)
+{
+    return new_empty_in_python(o, py::make_tuple(rows, columns), type);
 }
 
 // f() with its C++ exceptions as Python ones.  The calls below release the interpreter while they allocate and launch; a
@@ -389,17 +393,26 @@ PyObject *py_route_experts(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (PyErr_Occurred()) throw python_error();
         void *stream = PyLong_AsVoidPtr(a[10]);
         if (r.top_k <= 0 || r.top_k > E) return PyLong_FromLong(MIXLLM_EINVAL);
+        const int64_t k = r.top_k;
         at::Tensor out[5];
+        if (overrides_new_empty(a[0])) {
+            out[0] = new_empty_in_python(a[0], T, k, at::kInt);
+            out[1] = new_empty_in_python(a[0], T, k, at::kFloat);
+            out[2] = new_empty_in_python(a[0], py::make_tuple(E + 1), at::kInt);
+            out[3] = new_empty_in_python(a[0], py::make_tuple(T * k), at::kInt);
+            out[4] = new_empty_in_python(a[0], T, k, at::kInt);
+        }
         int rc;
         {
             py::gil_scoped_release no_gil;
-            const auto ints = logits.options().dtype(at::kInt);
-            const int64_t k = r.top_k;
-            out[0] = at::empty({T, k}, ints);
-            out[1] = at::empty({T, k}, logits.options().dtype(at::kFloat));
-            out[2] = at::empty({E + 1}, ints);
-            out[3] = at::empty({T * k}, ints);
-            out[4] = at::empty({T, k}, ints);
+            if (!out[0].defined()) {
+                const auto ints = logits.options().dtype(at::kInt);
+                out[0] = at::empty({T, k}, ints);
+                out[1] = at::empty({T, k}, logits.options().dtype(at::kFloat));
+                out[2] = at::empty({E + 1}, ints);
+                out[3] = at::empty({T * k}, ints);
+                out[4] = at::empty({T, k}, ints);
+            }
             const int64_t need = (int64_t)route_workspace(&r);
             at::Tensor ws;
             if (need) ws = at::empty({need}, logits.options().dtype(at::kByte));
@@ -466,6 +479,7 @@ PyObject *py_experts_linear(PyObject *, PyObject *const *a, Py_ssize_t n)
         void *stream = PyLong_AsVoidPtr(rest[FP16 ? 5 : 4]);
         const at::Device dev = current(x, "activations on the device");
         shaped(y, at::kHalf, {places, e.columns}, "out: fp16, assignments x outputs");
+        if (!y.defined() && overrides_new_empty(a[0])) y = new_empty_in_python(a[0], places, e.columns, at::kHalf);
         int rc;
         {
             py::gil_scoped_release no_gil;
@@ -502,6 +516,7 @@ PyObject *py_experts_combine(PyObject *, PyObject *const *a, Py_ssize_t n)
         shaped(residual, at::kHalf, {T, N}, "residual: fp16, of the result's shape");
         shaped(out, at::kHalf, {T, N}, "out: fp16, tokens x outputs");
         const at::Device dev = current(y, "y: an fp16 matrix on the device");
+        if (!out.defined() && overrides_new_empty(a[0])) out = new_empty_in_python(a[0], T, N, at::kHalf);
         int rc;
         {
             py::gil_scoped_release no_gil;
