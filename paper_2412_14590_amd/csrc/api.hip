@@ -182,7 +182,9 @@ int auto_path(const mixllm_desc &d, const LinearParams &p)
 
 // The same choice for a call with an epilogue.  The one decode kernel that has it is the evenly split one; decode
 // shapes beyond that (3 or 4 tokens of a K so long that they do not fit the LDS stage) take the tiled kernel, and so do
-// those of the kernel for a few dozen tokens beyond 32, where an epilogue does not fit its registers.
+// those of the kernel for a few dozen tokens beyond 32, where an epilogue does not fit its registers.  (The linear there and the tiled
+// kernel with silu, us: K = 8192, N = 10240, 33 to 64 tokens 26 and 27.5; K = 14336, N = 10240 40 and 47; K = 8192, N = 16384 36 and
+// 31; K = 16384, N = 20480 67 and 63.  With scratch the first two split K on either side: 25 and 25, 32 and 32.)
 int auto_path_epilogue(const mixllm_desc &d, const LinearParams &p)
 {
     const int path = auto_path(d, p);

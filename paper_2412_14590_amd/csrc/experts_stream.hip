@@ -427,12 +427,24 @@ __global__ __launch_bounds__(NT) void experts_stream_kernel(LinearParams p, Expe
 
 }  // namespace
 
+// Where this kernel takes the call: while the activations fit the registers they are quantized from (M K <= MAX_VALUES), but for more than
+// eight rows of K <= 2048 with one scale a row, where the quantizer's launch and the tiled kernel are ahead.  us, this kernel and those two,
+// 64 experts, weights from HBM, N = 4096 (1024):
+//   4 rows                                        8 rows                              32 rows
+//   K =  512    8.6 and  8.7  (8.0 and  7.8)       9.5 and  9.5  (8.2 and  8.6)       14.9 and 14.6  ( 9.9 and  9.0)
+//   K = 1408    9.8 and 10.9  (8.5 and 10.6)      12.7 and 12.1  (9.0 and 10.9)       23.8 and 22.5  (12.4 and 11.5)
+//   K = 2048   11.0 and 12.6  (8.8 and 11.8)      15.0 and 15.4  (9.2 and 12.0)       30.0 and 29.4  (14.0 and 13.0)
+//   K = 4096   14.4 and 18.8  (9.2 and 16.3)      21.1 and 24.4 (11.6 and 16.6)       50.6 and 53.8  (20.1 and 18.6)
+// K = 14336, one token of four experts 32.9 and 52.3; 64 rows of K = 1024 28.5 and 24.2, 128 rows 34.3 and 30.0.  With scales per 128
+// channels it is level or ahead at most sizes (K = 1408, 4, 8, 32 rows: 9.9 and 11.8, 12.8 and 13.2, 23.7 and 24.9; 16 to 64 rows of K <= 512 and N = 1024
+// 4 to 10 % behind).  A token's four experts of K = 4096, N = 2816 12.4 and 18.4, two tokens' 16.8 and 19.0, four tokens' 24.9 and 26.2.
 bool experts_stream_covers(const LinearParams &p, const ExpertsArgs &a)
 {
     // tiles of a part, in quarters, in 32 bits: every place may be a row tile of its own, and every expert may have all places in
     // lists that overlap
     const long tiles = std::max((long)a.places, (long)a.E * ((a.places + 15) / 16)) * ((p.N + 30) / 16 + 1);
-    return a.places <= MAX_PLACES && p.M <= MAX_PLACES && (size_t)p.M * p.K <= (size_t)MAX_VALUES && 4 * tiles < (1l << 31);
+    if (a.places > MAX_PLACES || p.M > MAX_PLACES || (size_t)p.M * p.K > (size_t)MAX_VALUES || 4 * tiles >= (1l << 31)) return false;
+    return !(p.act_per_token && a.places > 8 && p.K <= 2048);
 }
 
 int launch_experts_stream(const LinearParams &p, const ExpertsArgs &a, hipStream_t st)

@@ -37,17 +37,22 @@ def rounds_of(counts, layers, N):
     return (U8 // (WAVES * nb8) if nb8 else 0), (U4 // (WAVES * (B - nb8)) if B > nb8 else 0)
 
 
-# tokens, experts, k, K, N, shares of 8-bit channels, rounds of the 8-bit and of the 4-bit part (at least)
+# tokens, experts, k, K, N, shares of 8-bit channels, rounds of the 8-bit and of the 4-bit part (at least).  (With one scale a row
+# more than eight rows of a short K are the tiled kernel's: such cases are here for the scales per group.)
 CASES = {
-    "rounds and a rest": (8, 6, 4, 128, 16002, (0.1, 0.0, 0.3), (1, 1)),
-    "a change of batch": (16, 16, 8, 128, 16002, (0.1, 0.0, 0.3, 1.0, 0.2), (5, 5)),
+    "rounds and a rest": (2, 8, 4, 128, 16002, (0.1, 0.0, 0.3), (1, 1)),
+    "... of many rows": (8, 6, 4, 128, 16002, (0.1, 0.0, 0.3), (1, 1)),
+    "a change of batch": (1, 8, 8, 128, 40002, (0.1, 0.0, 0.3, 1.0, 0.2), (5, 5)),
+    "... of many rows, too": (16, 16, 8, 128, 16002, (0.1, 0.0, 0.3, 1.0, 0.2), (5, 5)),
     "three row tiles": (60, 3, 2, 128, 16002, (0.2, 0.05, 0.4), (2, 4)),
-    "ragged groups": (10, 9, 5, 640, 8194, (0.5, 0.0, 1.0), (1, 3)),
+    "ragged groups": (4, 8, 2, 640, 16002, (0.5, 0.0, 1.0), (1, 1)),
+    "many rows of a long K": (4, 20, 8, 4096, 2050, (0.1, 0.4), (0, 0)),
     "two lists of chunks": (1, 32, 32, 16256, 4112, (0.2, 0.0), (2, 4)),
-    "one part only": (16, 16, 8, 128, 16002, (0.0,), (0, 5)),
-    "the other part only": (16, 16, 8, 256, 8002, (1.0,), (2, 0)),
-    "more than 512 experts": (40, 700, 3, 128, 34, (0.1, 0.0, 1.0, 0.5), (0, 0)),
-    "1024 experts": (5, 1024, 20, 128, 66, (0.3, 1.0), (0, 0)),
+    "one part only": (1, 8, 8, 128, 40002, (0.0,), (0, 5)),
+    "the other part only": (1, 8, 8, 256, 22002, (1.0,), (5, 0)),
+    "more than 512 experts": (4, 700, 2, 128, 34, (0.1, 0.0, 1.0, 0.5), (0, 0)),
+    "1024 experts": (2, 1024, 4, 128, 66, (0.3, 1.0), (0, 0)),
+    "1024 experts, many rows": (5, 1024, 20, 128, 66, (0.3, 1.0), (0, 0)),
 }
 
 
