@@ -6,7 +6,8 @@ quantized linear runs in the library's own kernels.  There is no fallback: if th
 library is missing the import of `lib()` raises."""
 import ctypes as C
 import os
-from dataclasses import dataclass, replace
+from copy import copy
+from dataclasses import dataclass
 from typing import Optional
 
 import numpy as np
@@ -473,7 +474,7 @@ def pack_experts(layers) -> PackedExperts:
     d = first.desc()
     _check(lib().mixllm_experts_table(C.byref(d), len(layers), entries, _ptr(table), _stream()), "mixllm_experts_table")
     pairs = _all_keep_pairs(layers)
-    return PackedExperts(first.K, first.N, first.w8_group, tuple(replace(L) for L in layers), table, max(L.n8 for L in layers), pairs,
+    return PackedExperts(first.K, first.N, first.w8_group, tuple(copy(L) for L in layers), table, max(L.n8 for L in layers), pairs,
                          tuple(t for L in layers for t in (L.w4, L.w8, L.s4, L.s8, L.z4, L.perm)))
 
 
