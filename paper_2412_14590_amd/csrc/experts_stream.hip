@@ -16,11 +16,11 @@
 //    (of a tile of the rest: all waves', in wave order) become results in one loop.
 //  * The zero point is hoisted, sum a (q - z) = sum a q - z sum a, sum a from an MFMA against ones.  Scales per (token,
 //    group): their products with the weights' from one fp16 MFMA a group, in the accumulators' layout.
-// What comes before the first request (3.2 us of 10.5 for a token and 26 MB) is as much of the time on small layers as the weights:
-// every thread loads one expert's offsets and table entry at once, those with rows go into LDS one after another, and the lanes of a
-// wave then work out where its next 64 chunks lie, a chunk a lane; a request only reads that out of its lane.  With the search for a
-// chunk's expert in every request, a token's four experts of 13 / 26 MB took 12.3 / 13.9 us, now 10.4 / 12.0; the tiled
-// kernel and the quantizer take 10.7 / 17.5.  Two chunks in flight a wave: three and four 0.2 to 1.3 us more.
+// What comes before the first request (3.2 us by clock stamps, of the 11.4 of a token whose four experts have 26 MB) is as much of the
+// time on small layers as the weights: every thread loads one expert's offsets and table entry at once, those with rows go into LDS one
+// after another, and the lanes of a wave then work out where its next 64 chunks lie, a chunk a lane; a request only reads that out of
+// its lane.  With the search for a chunk's expert in every request a token took 1.9 us more.  Two chunks in flight a wave: three and four
+// 0.2 to 1.3 us more.  Against the quantizer and the tiled kernel: experts_stream_covers.
 #include <algorithm>
 #include <type_traits>
 

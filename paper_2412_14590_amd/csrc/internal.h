@@ -244,7 +244,7 @@ int cu_count();
 bool decode_can_fuse_quantizer(const LinearParams &p);
 int launch_linear_prefill(const LinearParams &p, hipStream_t st);
 bool prefill_covers(const LinearParams &p);
-// tiles cut along K over the waves of a block (linear_prefill.hip): where they pay, and the launch
+// tiles cut along K over the waves of a block (tiled.h): where they pay (linear_prefill.hip), and the launch
 bool slices_pay(const LinearParams &p);
 int launch_linear_slices(const LinearParams &p, hipStream_t st);
 void slices_plan(const LinearParams &p, int out[6]);
@@ -253,7 +253,7 @@ size_t prefill_scratch_bytes(const LinearParams &p);
 // true when the tiled kernel, given p.partials / p.partials_cap, would split K for `p`
 bool prefill_would_split(const LinearParams &p);
 bool prefill_plan(const LinearParams &p, int out[13]);
-// path for 17..128 tokens (linear_mid.hip)
+// path for 17..64 tokens (mid.h; which shapes it takes: linear_mid.hip)
 bool mid_covers(const LinearParams &p);
 int launch_linear_mid(const LinearParams &p, hipStream_t st);
 // the same kernels with an epilogue (p.ep); p.P and p.S are null

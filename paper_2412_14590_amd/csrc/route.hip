@@ -15,8 +15,9 @@
 // one block does it all in one launch; beyond, the first launch leaves the counts of every block and expert, and the
 // second adds up those of the blocks before its own.
 //
-// Bound by instructions and latency, not by the logits' few bytes: one token of 64 experts 3.8 us (one launch after the other), 61 tokens
-// of 256 in groups 12.3, 16384 tokens of 128 experts, 4 MB of logits, 16 (10 and 6 of the two launches).
+// Bound by instructions and latency, not by the logits' few bytes: one token of 64 experts 3.6 us (one launch after the other in a graph; a
+// call from Python takes the host 6.3 to 7.4, five result tensors among it), 61 tokens of 256 in groups 12.3, 16384 tokens of
+// 128 experts, 4 MB of logits, 16 (10 and 6 of the two launches).
 #include <algorithm>
 #include <type_traits>
 
