@@ -192,9 +192,9 @@ def _version(t: torch.Tensor):
 
 
 def _keeps_pairs(perm):
-    """Of an order with an even number of channels in either part (tensor or numpy array): every even place has an even channel,
-    and the place after it the next."""
-    return ((perm[0::2] % 2 == 0) & (perm[1::2] == perm[0::2] + 1)).all()
+    """Of orders [.., N] with an even number of channels in either part (tensor or numpy array): every even place has an even
+    channel, and the place after it the next."""
+    return ((perm[..., 0::2] % 2 == 0) & (perm[..., 1::2] == perm[..., 0::2] + 1)).all(-1)
 
 
 @dataclass
@@ -449,14 +449,16 @@ class PackedExperts:
 
 
 def _all_keep_pairs(layers) -> bool:
-    """PackedLayer.pairs of all of them, with one wait for the device."""
+    """PackedLayer.pairs of all of them (of one N), with one wait for the device."""
     if any(L.N % 2 or L.n8 % 2 for L in layers):
         return False
     new = [L for L in layers if L._seen is None]
     if new and new[0].perm.is_cuda and torch.cuda.is_current_stream_capturing():
         return False
     if new:
-        for L, keeps in zip(new, torch.stack([_keeps_pairs(L.perm) for L in new]).tolist()):
+        some = max(1, (1 << 24) // new[0].N)   # orders looked at together: 64 MB of copies
+        answers = [_keeps_pairs(torch.stack([L.perm for L in new[i:i + some]])) for i in range(0, len(new), some)]
+        for L, keeps in zip(new, torch.cat(answers).tolist()):
             L._seen = (L.perm, _version(L.perm), L.n8, keeps)
     return all(L.pairs for L in layers)
 

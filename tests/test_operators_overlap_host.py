@@ -1,4 +1,5 @@
-"""Operators next to the linear, without a GPU: results may lie on the residual, on nothing else that a call reads."""
+"""Operators next to the linear, without a GPU: results may lie on the residual, on nothing else that a call reads; and grids beyond a
+launch."""
 import ctypes as C
 
 import pytest
@@ -57,3 +58,12 @@ def test_sums_refuse_results_on_their_operands():
     assert f() == f(r=FAKE) == f(y=FAKE + T * row) == f(y=FAKE - places * row) == f(r=FAKE + T * row) == EHIP
     for bad in (dict(y=FAKE), dict(y=FAKE + (T - 1) * row), dict(y=FAKE - (places - 1) * row), dict(w=FAKE + 4), dict(s=FAKE - 4), dict(r=FAKE + 16)):
         assert f(**bad) == EINVAL, bad
+
+
+def test_grids_that_cannot_be_launched_are_refused():
+    # 1024 experts with a row each, 2^23 channels: 2^26 tiles
+    e, L, address = binding._Epilogue(None, None, 0, 0), mx.lib(), W
+    d = binding._desc(1024, 128, 1 << 23, 0)
+    y = 0x7f0000000000
+    assert L.mixllm_experts_linear(C.byref(d), 1024, address, address, address, address, address, 1, C.byref(e), y, None) == -2
+    assert L.mixllm_experts_linear_fp16(C.byref(d), 1024, address, address, address, address, 1, C.byref(e), y, address, 1 << 24, None) == -2
