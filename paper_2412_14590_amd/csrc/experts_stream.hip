@@ -429,7 +429,7 @@ __global__ __launch_bounds__(NT) void experts_stream_kernel(LinearParams p, Expe
 
 // Where this kernel takes the call: while the activations fit the registers they are quantized from (M K <= MAX_VALUES), but for more than
 // eight rows of K <= 2048 with one scale a row, where the quantizer's launch and the tiled kernel are ahead.  us, this kernel and those two,
-// 64 experts, weights from HBM, N = 4096 (1024):
+// 64 experts, other ones from call to call, N = 4096 (1024):
 //   4 rows                                        8 rows                              32 rows
 //   K =  512    8.6 and  8.7  (8.0 and  7.8)       9.5 and  9.5  (8.2 and  8.6)       14.9 and 14.6  ( 9.9 and  9.0)
 //   K = 1408    9.8 and 10.9  (8.5 and 10.6)      12.7 and 12.1  (9.0 and 10.9)       23.8 and 22.5  (12.4 and 11.5)
